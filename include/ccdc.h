@@ -299,6 +299,115 @@ int ccdc_pipeline_fused_noalloc(const ccdc_plan_t *plan, const void *V, void *X,
 int ccdc_node_encode(const ccdc_plan_t *plan, int node, const void *V, void *X, void *stream);
 int ccdc_node_decode_reduce(const ccdc_plan_t *plan, int node, const void *V, const void *X, void *Phi, void *stream);
 
+/*
+ * A trained block to map: a residual block of a network whose per-file gradients are intermediate values.
+ * ccdc_map stands in for the paper's free g_q; these calls are a g_q that a training job has.  A batch is the
+ * M tokens of N files, one file after the other, as rows of matrices; what is learned has one gradient per
+ * file, written with a stride, so that it can go straight into the rows of V (V[n] = [Q][T] of file n).  Every
+ * gradient depends on the file's own rows, its number and its tokens' places in it alone, and every sum has one order:
+ * the r nodes that store a file make the same bits of it, in whatever batch, which is what cancelling side
+ * information rests on.
+ *
+ *   ffn      a = x Wg', u = x Wu', h = D(act(a) u), y = h Wd'   (W_in = [Wg; Wu]: [2 hidden][width],
+ *            W_out = Wd: [width][hidden]; ' is the transpose)
+ *   join     y = residual_scale x + gate D(norm(f; w_post)),  n = norm(y; w_pre):  the end of one block and
+ *            the beginning of the next.  norm(v; w) = w v / sqrt(mean(v^2) + eps), of v - mean(v) where centred.
+ *   dropout  y = D(x) + residual
+ *
+ * D, dropout with probability p: element (row, column c) of token t of the file with number id is kept where
+ * halfword c % 8 (word (c % 8) / 2, low half first) of Philox4x32-10 (Salmon, Moraes, Dror, Shaw 2011) on the
+ * counter (c / 8, t, id, site) and the key (low, high half of seed) is at least thr = rint(65536 p), and
+ * multiplied by 65536 / (65536 - thr); thr = 65536 keeps nothing.  site tells apart the masks of one step:
+ * 2 layer for h, 2 layer + 1 for a join.  No mask is stored; the gradient calls make it again from the same seed.
+ *
+ * Elements are those of the mode (fp32 for CCDC_F32_SUM and CCDC_F32_SUM_XOR, bfloat16, binary16); CCDC_U32_XOR
+ * has no products and is refused.  Sums, norms and activations are carried in fp32; results are rounded once, to
+ * nearest even.  In the 16-bit modes h and the gradients of a and u are rounded to the mode's format between the
+ * products that make and those that take them; in fp32 the products are exact to 2^-24 or so.
+ * Matrices are row-major with a row stride in elements (ld...), at least their width, columns contiguous; any
+ * alignment to the element is taken.
+ */
+typedef struct ccdc_block_s ccdc_block_t;       /* opaque, owned by the library */
+
+enum ccdc_activation { CCDC_ACT_SILU = 0, CCDC_ACT_GELU = 1 /* erf form */, CCDC_ACT_RELU = 2 };
+enum ccdc_norm { CCDC_NORM_RMS = 0, CCDC_NORM_CENTRED = 1 };
+
+typedef struct ccdc_block_config {
+    int64_t width, hidden;         /* 1 .. 2^20 each */
+    int32_t mode;                  /* enum ccdc_mode */
+    int32_t activation;            /* enum ccdc_activation */
+    int32_t norm;                  /* enum ccdc_norm */
+    uint32_t layer;                /* number of the block, below 2^31 */
+    float eps;                     /* > 0 */
+    float residual_scale;
+    float dropout_hidden;          /* 0 .. 1 */
+    float dropout_out;             /* 0 .. 1 */
+} ccdc_block_config;
+
+enum ccdc_block_query {
+    CCDC_BLOCK_Q_TOKENS = 0,       /* M; needs a bound block, as what follows */
+    CCDC_BLOCK_Q_FILES,            /* N */
+    CCDC_BLOCK_Q_SAVED_BYTES,      /* what ccdc_ffn_forward keeps for ccdc_ffn_backward */
+    CCDC_BLOCK_Q_WORKSPACE_BYTES   /* device bytes that ccdc_block_upload allocates besides tables */
+};
+
+/* Host only: checks and keeps the configuration.  CCDC_EINVAL for a value out of range or CCDC_U32_XOR. */
+int ccdc_block(const ccdc_block_config *config, ccdc_block_t **out);
+void ccdc_block_destroy(ccdc_block_t *block);   /* NULL is fine */
+
+/* Fix the batch: files files of tokens[n] >= 0 tokens each and, for the masks, their numbers ids[n] (NULL: 0, 1,
+ * ...; for one node of a plan, CCDC_Q_NODE_FILES).  Host only; drops any device tables.  CCDC_EINVAL for files < 1, a
+ * negative length or number; CCDC_ESIZE when tokens or a launch would pass 2^31-1 or a buffer 2^40 bytes. */
+int ccdc_block_bind(ccdc_block_t *block, int files, const int64_t *tokens, const int32_t *ids);
+
+/* Copy the tables to the CURRENT HIP device and allocate the workspace there.  As ccdc_plan_upload. */
+int ccdc_block_upload(ccdc_block_t *block);
+int ccdc_block_query(const ccdc_block_t *block, int what, void *out, size_t out_bytes);
+
+/*
+ * The calls below need an uploaded block (CCDC_ESTATE otherwise) and its device to be current.  They only enqueue
+ * kernels on `stream` and allocate nothing; those that use the block's workspace are put in order across streams as the
+ * plan's are.  CCDC_EINVAL for a null pointer (where NULL has no meaning given), one not aligned to the element,
+ * a stride below the width, rows outside 0..M.  Outputs are written in full and overlap no input unless that is said.
+ *
+ * rows: the first `rows` rows of the batch are computed (a program that answers binds the most it meets and
+ * passes what it has); training passes M.  0 rows are nothing to do.
+ */
+
+/* y [rows][width] from x [rows][width].  saved: NULL, or CCDC_BLOCK_Q_SAVED_BYTES bytes, aligned to 16, for the
+ * backward call (then rows must be M). */
+int ccdc_ffn_forward(const ccdc_block_t *block, int64_t rows, const void *x, int64_t ldx, const void *W_in,
+                     const void *W_out, void *y, int64_t ldy, void *saved, uint64_t seed, void *stream);
+
+/* From dy, the gradient of y: dx, and file by file dW_in[n] = dW_in + n ld_in ([2 hidden][width], contiguous) and
+ * dW_out[n] = dW_out + n ld_out ([width][hidden]).  saved is only read.  dx may be dy (then lddx = lddy); a file without tokens has
+ * zeros.  dx or both dW may be NULL: not wanted. */
+int ccdc_ffn_backward(const ccdc_block_t *block, const void *x, int64_t ldx, const void *W_in, const void *W_out,
+                      const void *saved, const void *dy, int64_t lddy, void *dx, int64_t lddx, void *dW_in,
+                      int64_t ld_in, void *dW_out, int64_t ld_out, void *stream);
+
+/* The join.  f NULL: y = residual_scale x and no gate; n NULL: without the norm after it; y NULL: only n.  w_post, w_pre NULL: ones;
+ * gate NULL: one, else [width], the same for every file (ld_gate 0), or a row per file (ld_gate >= width).
+ * All matrices have row stride ld.  y may be x or f; n may be x or f. */
+int ccdc_join_forward(const ccdc_block_t *block, int64_t rows, const void *x, const void *f, const void *w_post,
+                      const void *gate, int64_t ld_gate, const void *w_pre, void *y, void *n, int64_t ld,
+                      uint64_t seed, void *stream);
+
+/* From dn, the gradient of n (NULL: there is no n), and dr, the gradient that reaches y by other ways (NULL: none;
+ * not both NULL): dx and df (NULL with f), and file by file dw_post, dgate, dw_pre (rows of `width` elements, ld_file
+ * apart; NULL: not wanted).  y as ccdc_join_forward stored it (needed with dn).  A gate shared by the files has its
+ * gradient file by file like everything else.  dx may be dr or dn; df may be f, or dn or dr where dx is not. */
+int ccdc_join_backward(const ccdc_block_t *block, const void *dn, const void *dr, const void *y, const void *f,
+                       const void *w_post, const void *gate, int64_t ld_gate, const void *w_pre, void *dx, void *df,
+                       int64_t ld, void *dw_post, void *dgate, void *dw_pre, int64_t ld_file, uint64_t seed,
+                       void *stream);
+
+/* y = D(x) + residual (NULL: 0) on rows rows of `columns` elements, probability p; also its own gradient.  y may be
+ * x or residual (with the same stride). */
+int ccdc_dropout(const ccdc_block_t *block, int64_t rows, int64_t columns, double p, uint32_t site, uint64_t seed,
+                 const void *x, int64_t ldx, const void *residual, int64_t ld_residual, void *y, int64_t ldy,
+                 void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -6,8 +6,10 @@ library; the first use does, and fails loudly if it has not been built.
 """
 from . import binding  # noqa: F401
 from .binding import (  # noqa: F401
+    Block,
     CcdcError,
     Plan,
+    ccdc_block,
     ccdc_plan,
     ccdc_plan_compression,
     ccdc_plan_jobs,

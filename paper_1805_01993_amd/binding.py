@@ -28,12 +28,28 @@ ELEM_BYTES = {F32_SUM: 4, U32_XOR: 4, F32_SUM_XOR: 4, BF16_SUM_XOR: 2, F16_SUM_X
  Q_ROWS_PER_NODE, Q_NODE_ROWS, Q_FILE_NODES, Q_FILES_PER_NODE, Q_NODE_FILES, Q_PIPELINE_LAUNCH,
  Q_REDUCE_LAUNCH) = range(128, 142)
 
+# enum ccdc_activation, ccdc_norm, ccdc_block_query
+ACT_SILU, ACT_GELU, ACT_RELU = range(3)
+ACTIVATIONS = {"silu": ACT_SILU, "gelu": ACT_GELU, "relu": ACT_RELU}
+NORM_RMS, NORM_CENTRED = range(2)
+NORMS = {"rms": NORM_RMS, "centred": NORM_CENTRED}
+BLOCK_Q_TOKENS, BLOCK_Q_FILES, BLOCK_Q_SAVED_BYTES, BLOCK_Q_WORKSPACE_BYTES = range(4)
+
 EXPORTS = [
     "ccdc_plan", "ccdc_plan_jobs", "ccdc_plan_jobs_repeated", "ccdc_plan_compression", "ccdc_plan_destroy", "ccdc_plan_bind", "ccdc_plan_upload",
     "ccdc_plan_query", "ccdc_strerror", "ccdc_map", "ccdc_combine", "ccdc_encode", "ccdc_decode", "ccdc_reduce",
     "ccdc_shuffle_fused", "ccdc_pipeline_fused", "ccdc_pipeline_fused_noalloc", "ccdc_node_encode",
     "ccdc_node_decode_reduce",
+    "ccdc_block", "ccdc_block_destroy", "ccdc_block_bind", "ccdc_block_upload", "ccdc_block_query",
+    "ccdc_ffn_forward", "ccdc_ffn_backward", "ccdc_join_forward", "ccdc_join_backward", "ccdc_dropout",
 ]
+
+
+class BlockConfig(C.Structure):
+    """ccdc_block_config."""
+    _fields_ = [("width", C.c_int64), ("hidden", C.c_int64), ("mode", C.c_int32), ("activation", C.c_int32),
+                ("norm", C.c_int32), ("layer", C.c_uint32), ("eps", C.c_float), ("residual_scale", C.c_float),
+                ("dropout_hidden", C.c_float), ("dropout_out", C.c_float)]
 
 
 # What the native marshalling (csrc/marshal.cpp) calls: entry point, whether a node number comes first, its tensors.
@@ -98,6 +114,20 @@ def load_library():
         fn = getattr(lib, name)
         fn.restype = C.c_int
         fn.argtypes = [vp, C.c_int] + [vp] * nptr + [vp]
+    i32, u64 = C.c_int32, C.c_uint64
+    for name, args in (("ccdc_block", [C.POINTER(BlockConfig), C.POINTER(vp)]), ("ccdc_block_upload", [vp]),
+                       ("ccdc_block_bind", [vp, C.c_int, C.POINTER(i64), C.POINTER(i32)]),
+                       ("ccdc_block_query", [vp, C.c_int, vp, C.c_size_t]),
+                       ("ccdc_ffn_forward", [vp, i64, vp, i64, vp, vp, vp, i64, vp, u64, vp]),
+                       ("ccdc_ffn_backward", [vp, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
+                       ("ccdc_join_forward", [vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, i64, u64, vp]),
+                       ("ccdc_join_backward", [vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp, vp, vp, i64, u64, vp]),
+                       ("ccdc_dropout", [vp, i64, i64, C.c_double, C.c_uint32, u64, vp, i64, vp, i64, vp, i64, vp])):
+        fn = getattr(lib, name)
+        fn.restype = C.c_int
+        fn.argtypes = args
+    lib.ccdc_block_destroy.restype = None
+    lib.ccdc_block_destroy.argtypes = [vp]
     _load_marshal(lib)
     _lib = lib
     return lib
@@ -401,6 +431,178 @@ class Plan:
         _check(self._lib.ccdc_node_decode_reduce(self._h, int(node), self._need(V, "V", "V"), self._need(X, "X", "X"),
                                                  self._need(Phi, "Phi", "Phi"), _stream_ptr(stream)),
                "ccdc_node_decode_reduce")
+
+
+class Block:
+    """Owns one ccdc_block_t: a residual block whose per-file gradients are intermediate values.  Methods mirror the C
+    entry points (include/ccdc.h has the formulas).
+
+    Matrices are tensors [rows][columns] of the mode's type with contiguous columns, parameters contiguous.  Gradients of
+    parameters have the file as their first dimension, with any stride, as views of V's rows have (the three of a join the
+    same).  Calls are asynchronous on `stream`, default torch's current stream."""
+
+    def __init__(self, width, hidden, mode, activation="silu", norm="rms", eps=1e-6, residual_scale=1.0,
+                 dropout_hidden=0.0, dropout_out=0.0, layer=0):
+        self._h = None
+        lib = load_library()
+        mode = MODES.get(mode, mode)
+        config = BlockConfig(int(width), int(hidden), mode, ACTIVATIONS.get(activation, activation), NORMS.get(norm, norm),
+                             int(layer), eps, residual_scale, dropout_hidden, dropout_out)
+        h = C.c_void_p()
+        _check(lib.ccdc_block(C.byref(config), C.byref(h)), "ccdc_block")
+        import torch
+        self._h, self._lib = h, lib
+        self.width, self.hidden = int(width), int(hidden)
+        self.dtype = {BF16_SUM_XOR: torch.bfloat16, F16_SUM_XOR: torch.float16}.get(mode, torch.float32)
+        self.tokens = self.files = self.saved_bytes = None
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.ccdc_block_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def bind(self, tokens, ids=None):
+        """The batch: tokens of each file and, for the dropout masks, the files' numbers (default 0, 1, ...)."""
+        tokens = [int(t) for t in tokens]
+        if ids is not None and len(ids) != len(tokens):
+            raise ValueError("ids: need one number a file")
+        numbers = None if ids is None else (C.c_int32 * len(tokens))(*(int(i) for i in ids))
+        _check(self._lib.ccdc_block_bind(self._h, len(tokens), (C.c_int64 * len(tokens))(*tokens), numbers), "ccdc_block_bind")
+        self.tokens, self.files = self.query(BLOCK_Q_TOKENS), self.query(BLOCK_Q_FILES)
+        self.saved_bytes = self.query(BLOCK_Q_SAVED_BYTES)
+        return self
+
+    def upload(self):
+        _check(self._lib.ccdc_block_upload(self._h), "ccdc_block_upload")
+        return self
+
+    def query(self, what):
+        v = C.c_int64()
+        _check(self._lib.ccdc_block_query(self._h, what, C.byref(v), 8), f"ccdc_block_query({what})")
+        return int(v.value)
+
+    # ---- tensors
+    def _matrix(self, t, name, columns, rows=None):
+        """Address of a matrix with contiguous columns (None: null)."""
+        if t is None:
+            return None
+        if not t.is_cuda or t.dtype != self.dtype:
+            raise ValueError(f"{name}: need a device tensor of {self.dtype}, got {t.dtype} on {t.device}")
+        if t.dim() != 2 or t.shape[1] != columns or (rows is not None and t.shape[0] != rows):
+            raise ValueError(f"{name}: need {[rows if rows is not None else 'rows', columns]}, got {list(t.shape)}")
+        if (columns > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < columns):
+            raise ValueError(f"{name}: need contiguous columns in rows that do not overlap")
+        return t.data_ptr()
+
+    @staticmethod
+    def _ld(t):
+        """Row stride; a matrix of one row may say anything there."""
+        return 0 if t is None else max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+    def _same_ld(self, *tensors):
+        strides = {self._ld(t) for t in tensors if t is not None and t.shape[0] > 1}
+        if len(strides) > 1:
+            raise ValueError("the matrices of a join need the same row stride")
+        return strides.pop() if strides else self.width
+
+    def _parameter(self, t, name, *shape):
+        if t is None:
+            return None
+        if not t.is_cuda or t.dtype != self.dtype:
+            raise ValueError(f"{name}: need a device tensor of {self.dtype}, got {t.dtype} on {t.device}")
+        if tuple(t.shape) != shape or not t.is_contiguous():
+            raise ValueError(f"{name}: need {list(shape)}, contiguous, got {list(t.shape)}")
+        return t.data_ptr()
+
+    def _gradients(self, named):
+        """Addresses of per-file gradients, and their common file stride."""
+        ptrs, strides = [], set()
+        for name, t, shape in named:
+            if t is None:
+                ptrs.append(None)
+                continue
+            if not t.is_cuda or t.dtype != self.dtype:
+                raise ValueError(f"{name}: need a device tensor of {self.dtype}, got {t.dtype} on {t.device}")
+            if tuple(t.shape) != (self.files,) + shape or not t[0].is_contiguous():
+                raise ValueError(f"{name}: need {[self.files, *shape]}, a file's part contiguous, got {list(t.shape)}")
+            if self.files > 1:
+                strides.add(t.stride(0))
+            ptrs.append(t.data_ptr())
+        if len(strides) > 1:
+            raise ValueError("the gradients of a call need the same stride from file to file")
+        return ptrs, strides.pop() if strides else 0
+
+    # ---- the block
+    def ffn_forward(self, x, W_in, W_out, y, saved=None, seed=0, stream=None):
+        """y = D(act(x Wg') x Wu') Wd'.  saved: a uint8 tensor of saved_bytes for ffn_backward."""
+        rows = x.shape[0]
+        if saved is not None and (not saved.is_cuda or not saved.is_contiguous() or saved.numel() * saved.element_size() < self.saved_bytes):
+            raise ValueError(f"saved: need {self.saved_bytes} contiguous bytes on the device")
+        _check(self._lib.ccdc_ffn_forward(
+            self._h, rows, self._matrix(x, "x", self.width), self._ld(x),
+            self._parameter(W_in, "W_in", 2 * self.hidden, self.width), self._parameter(W_out, "W_out", self.width, self.hidden),
+            self._matrix(y, "y", self.width, rows), self._ld(y), None if saved is None else saved.data_ptr(), seed,
+            _stream_ptr(stream)), "ccdc_ffn_forward")
+
+    def ffn_backward(self, x, W_in, W_out, saved, dy, dx, dW_in, dW_out, stream=None):
+        """dx and, file by file, dW_in [files][2 hidden][width] and dW_out [files][width][hidden]; dx or both dW None: not
+        wanted."""
+        if not saved.is_cuda or not saved.is_contiguous() or saved.numel() * saved.element_size() < self.saved_bytes:
+            raise ValueError(f"saved: need {self.saved_bytes} contiguous bytes on the device")
+        (din,), ld_in = self._gradients((("dW_in", dW_in, (2 * self.hidden, self.width)),))
+        (dout,), ld_out = self._gradients((("dW_out", dW_out, (self.width, self.hidden)),))
+        M = self.tokens
+        _check(self._lib.ccdc_ffn_backward(
+            self._h, self._matrix(x, "x", self.width, M), self._ld(x),
+            self._parameter(W_in, "W_in", 2 * self.hidden, self.width), self._parameter(W_out, "W_out", self.width, self.hidden),
+            saved.data_ptr(), self._matrix(dy, "dy", self.width, M), self._ld(dy), self._matrix(dx, "dx", self.width, M),
+            self._ld(dx), din, ld_in, dout, ld_out, _stream_ptr(stream)), "ccdc_ffn_backward")
+
+    def _gate(self, gate):
+        if gate is None or gate.dim() == 1:
+            return self._parameter(gate, "gate", self.width), 0
+        return self._matrix(gate, "gate", self.width, self.files), self._ld(gate)
+
+    def join_forward(self, x, f, y, n, w_post=None, gate=None, w_pre=None, seed=0, stream=None):
+        """y = residual_scale x + gate D(norm(f; w_post)), n = norm(y; w_pre).  f, y, n None: without it; gate [width], or
+        [files][width]."""
+        d, rows = self.width, x.shape[0]
+        g, ld_gate = self._gate(gate)
+        _check(self._lib.ccdc_join_forward(
+            self._h, rows, self._matrix(x, "x", d), self._matrix(f, "f", d, rows), self._parameter(w_post, "w_post", d), g,
+            ld_gate, self._parameter(w_pre, "w_pre", d), self._matrix(y, "y", d, rows), self._matrix(n, "n", d, rows),
+            self._same_ld(x, f, y, n), seed, _stream_ptr(stream)), "ccdc_join_forward")
+
+    def join_backward(self, dn, dr, y, f, dx, df, w_post=None, gate=None, w_pre=None, dw_post=None, dgate=None, dw_pre=None,
+                      seed=0, stream=None):
+        """From dn, the gradient of n, and dr, that of y by other ways: dx, df and per-file gradients [files][width]."""
+        d, M = self.width, self.tokens
+        g, ld_gate = self._gate(gate)
+        grads, ld = self._gradients((("dw_post", dw_post, (d,)), ("dgate", dgate, (d,)), ("dw_pre", dw_pre, (d,))))
+        _check(self._lib.ccdc_join_backward(
+            self._h, self._matrix(dn, "dn", d, M), self._matrix(dr, "dr", d, M), self._matrix(y, "y", d, M),
+            self._matrix(f, "f", d, M), self._parameter(w_post, "w_post", d), g, ld_gate, self._parameter(w_pre, "w_pre", d),
+            self._matrix(dx, "dx", d, M), self._matrix(df, "df", d, M), self._same_ld(dn, dr, y, f, dx, df), *grads, ld, seed,
+            _stream_ptr(stream)), "ccdc_join_backward")
+
+    def dropout(self, x, y, p, site, seed=0, residual=None, stream=None):
+        """y = D(x) + residual; the gradient of x is the same call on that of y."""
+        rows, columns = x.shape
+        _check(self._lib.ccdc_dropout(
+            self._h, rows, columns, p, site, seed, self._matrix(x, "x", columns), self._ld(x),
+            self._matrix(residual, "residual", columns, rows), self._ld(residual), self._matrix(y, "y", columns, rows),
+            self._ld(y), _stream_ptr(stream)), "ccdc_dropout")
+
+
+def ccdc_block(width, hidden, mode, **config):
+    """A residual block (gated feed-forward, norms, gate, dropout) whose per-file gradients are rows of V."""
+    return Block(width, hidden, mode, **config)
 
 
 def ccdc_plan(K, r, Q, N):

@@ -1,0 +1,72 @@
+// A trained block (ccdc_block): its configuration, the batch it is bound to, and what its calls share.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+#include <mutex>
+#include <vector>
+
+#include "ccdc.h"
+
+namespace ccdc {
+
+// What a row of the batch belongs to: the numbers that its dropout masks are made from.
+struct RowOf {
+    int32_t id, token, file;          // the file's number, the token's place in it, the file's place in the batch
+};
+
+// Consecutive rows of one file, of which one workgroup sums what is learned.
+struct Chunk {
+    int32_t file, first, rows;
+};
+// 32 rows of 2048 bf16 values are four wavefronts' work for some 25 us; the sums of a chunk, written and read once
+// more, are 4 % of what its rows move.  The same for every batch: the order of a file's sums is its own.
+constexpr int kChunkRows = 32;
+constexpr int64_t kJoinWidth = 16384;         // widest rows that one workgroup holds in registers
+
+constexpr int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
+
+}  // namespace ccdc
+
+struct ccdc_block_s {
+    ccdc_block_config c{};
+    int elem = 4;                     // bytes of an element
+    int planes = 1;                   // 16-bit numbers that an operand of a product is held in
+
+    bool bound = false;
+    int64_t M = 0;                    // tokens of the batch
+    int N = 0;
+    int64_t hidden_ld = 0, width_ld = 0;          // row strides of the block's own matrices: whole packs of 16 bytes
+    std::vector<int32_t> first;       // [N + 1] rows the files begin at
+    std::vector<int32_t> ids;         // [N]
+    std::vector<ccdc::RowOf> row_of;  // [M]
+    std::vector<ccdc::Chunk> chunks;
+    std::vector<int32_t> chunk_first; // [N + 1]
+
+    // bytes from the workspace's beginning: hidden values; gradients of a and u; x, dy, W_in and W_out where products do
+    // not take them as they are; sums of the chunks (over all of these)
+    size_t at_h = 0, at_dau = 0, at_x = 0, at_dy = 0, at_in = 0, at_out = 0, workspace_bytes = 0;
+    size_t saved_h = 0, saved_p = 0, saved_q = 0, saved_bytes = 0;
+
+    bool uploaded = false;
+    int device = -1;
+    int32_t *d_first = nullptr, *d_chunk_first = nullptr;
+    ccdc::RowOf *d_row_of = nullptr;
+    ccdc::Chunk *d_chunks = nullptr;
+    void *d_workspace = nullptr;
+
+    // as a plan's (plan.hpp)
+    mutable std::mutex ws_mutex;
+    mutable void *ws_event = nullptr;
+    mutable void *ws_stream = nullptr;
+    mutable bool ws_used = false;
+};
+
+namespace ccdc {
+
+// The thresholds of 16-bit random numbers below which dropout takes a value out.
+inline uint32_t dropout_threshold(double p) { return (uint32_t)(p * 65536.0 + 0.5); }
+
+int bind_block(ccdc_block_t *b, int files, const int64_t *tokens, const int32_t *ids);
+
+}  // namespace ccdc

@@ -699,7 +699,7 @@ int reduce_chunks(const ccdc_plan_t *p, void *Phi, int split, int64_t chunk_stri
     return launched();
 }
 
-// The plan's workspace holds partial sums between the two kernels of one call.
+// The plan's workspace holds partial sums between the two kernels of one call (a block's, what one of its kernels makes for the next).
 // Calls that use it are put in order also when they come on different streams:
 // the plan remembers the stream of the last such call, and a call that arrives
 // on another stream first records the plan's event at the tail of that earlier
@@ -710,9 +710,10 @@ int reduce_chunks(const ccdc_plan_t *p, void *Phi, int split, int64_t chunk_stri
 // and forgotten (an event recorded outside a capture cannot be waited for
 // inside one): whoever replays the graph keeps it apart from other users of
 // the plan.  The earlier stream must still exist when the later call comes.
+template <class Owner>
 class WorkspaceOrder {
 public:
-    WorkspaceOrder(const ccdc_plan_t *p, hipStream_t st, bool uses_workspace)
+    WorkspaceOrder(const Owner *p, hipStream_t st, bool uses_workspace)
         : p_(p), st_(st), on_(uses_workspace && p->ws_event != nullptr)
     {
         if (!on_) return;
@@ -744,7 +745,7 @@ public:
     WorkspaceOrder &operator=(const WorkspaceOrder &) = delete;
 
 private:
-    const ccdc_plan_t *p_;
+    const Owner *p_;
     hipStream_t st_;
     bool on_;
 };
