@@ -13,7 +13,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libccdc.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 SOURCES = ["ccdc.hip", "pipeline.hip", "node.hip", "noalloc.hip", "map.hip", "receive.hip", "plan.cpp",
-           "block.cpp", "block.hip", "ffn.hip", "join.hip", "product.hip"]
+           "block.cpp", "block.hip", "few.hip", "ffn.hip", "join.hip", "product.hip"]
 # pipeline.hip has hundreds of kernel instantiations: it is compiled in pieces, two per payload algebra; receive.hip and node.hip in one each,
 # product.hip in one per element type
 PIECES = {"pipeline.hip": ("CCDC_PIPELINE_PART", 10), "receive.hip": ("CCDC_RECEIVE_PART", 5), "node.hip": ("CCDC_NODE_PART", 5),

@@ -76,6 +76,9 @@ int forward(const ccdc_block_t *b, int64_t rows, const void *x, int64_t ldx, con
             void *saved, uint64_t seed, hipStream_t st)
 {
     const int64_t d = b->c.width, F = b->c.hidden;
+    const Dropout drop = make_dropout(b->c.dropout_hidden, 2 * b->c.layer, seed);
+    if (!saved && rows <= kFewRows)
+        return few_forward(b, rows, x, ldx, W_in, W_out, y, ldy, inside_of(b->d_workspace, b->at_h), drop, st);
     const Prepared in = prepare(b, W_in, d, 2 * F, d, b->at_in, st), px = prepare(b, x, ldx, rows, d, b->at_x, st);
     const Prepared out = prepare(b, W_out, F, d, F, b->at_out, st);
     for (int rc : {in.rc, px.rc, out.rc})
@@ -87,7 +90,7 @@ int forward(const ccdc_block_t *b, int64_t rows, const void *x, int64_t ldx, con
     a.h = h;
     a.P = saved ? inside_of<float>(saved, b->saved_p) : nullptr;
     a.Q = saved ? inside_of<float>(saved, b->saved_q) : nullptr;
-    a.drop = make_dropout(b->c.dropout_hidden, 2 * b->c.layer, seed);
+    a.drop = drop;
     int rc = run_product(b->c.mode, Product::gated, a, st);
     if (rc != CCDC_OK) return rc;
     a = common(b);

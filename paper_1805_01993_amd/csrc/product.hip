@@ -31,7 +31,6 @@ typedef __bf16 Bf8 __attribute__((ext_vector_type(8)));
 typedef _Float16 Half8 __attribute__((ext_vector_type(8)));
 #define CCDC_LDS __attribute__((address_space(3)))
 
-constexpr int kStep = 64;         // k of a step
 
 __device__ const uint32_t zeros[4] = {};       // what is read in place of k past the end
 
@@ -56,16 +55,20 @@ __device__ __forceinline__ void copy_to_lds(uint32_t to, const void *from)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(to), "v"(from) : "memory");
 }
 
-// Bytes in LDS of pack `pack` (eight k) of row `row`, k contiguous: the eight rows that are read together are in different banks.
-__device__ __forceinline__ uint32_t contiguous_at(uint32_t row, uint32_t pack) { return row * 128 + ((pack ^ (row & 7)) * 16); }
+// Place in its row of pack `pack` (eight k) of row `row`, k contiguous, `packs` of them a row: sixteen rows are read together, and the
+// banks hold 16 / packs of them beside one another, so each so many rows have an order of their own.
+template <uint32_t packs>
+__device__ __forceinline__ uint32_t contiguous_pack(uint32_t row, uint32_t pack) { return pack ^ (row / (16 / packs) % packs); }
 // Place in its row of pack `pack` (eight rows of the side) at k, strided: the four k that are read together, 32 rows of
 // the side each, are in different banks.
 __device__ __forceinline__ uint32_t strided_pack(uint32_t k, uint32_t pack) { return pack ^ ((k & 3) << 2); }
 
-// The copies of one side that a wavefront makes in each step.
-template <bool STRIDED, int ROWS, int THREADS>
+// The copies of one side that a wavefront makes in each step of STEP k.
+template <bool STRIDED, int ROWS, int THREADS, int STEP>
 struct Copies {
-    static constexpr int count = ROWS * 8 / THREADS;
+    static constexpr bool strided = STRIDED;
+    static constexpr int count = ROWS * (STEP / 8) / THREADS;
+    static constexpr uint32_t packs = STRIDED ? ROWS / 8 : STEP / 8;      // of a row in LDS
     const uint16_t *base[count];          // the same for all lanes
     uint32_t offset[count];               // bytes, a lane's own
     uint32_t to;                          // byte in LDS of the first
@@ -80,47 +83,42 @@ struct Copies {
         for (int i = 0; i < count; i++) {
             const uint32_t p = i * THREADS + wave * 64;       // the first lane's pack
             if constexpr (STRIDED) {
-                constexpr uint32_t packs = ROWS / 8;
                 const uint32_t k = (p + lane) / packs, pack = strided_pack(k, (p + lane) % packs);
                 const int32_t column = min(row0 + (int32_t)pack * 8, s.columns - 8) - row0;
                 base[i] = s.p + row0;
                 offset[i] = (uint32_t)((k * s.ld + column) * 2);
             } else {
-                int32_t r = p / 8, second = 0;
+                int32_t r = p / packs, second = 0;
                 if constexpr (GATED) {
                     second = r / 32 % 2;
                     r = r / 64 * 32 + r % 32;
                 }
                 const int32_t from = min(row0 + r, rows - 1);
-                const uint32_t row = p / 8 + lane / 8;        // in LDS
-                const int32_t at = min(from + (int32_t)(lane / 8), rows - 1) - from;
+                const uint32_t row = (p + lane) / packs;      // in LDS
+                const int32_t at = min(from + (int32_t)(lane / packs), rows - 1) - from;
                 base[i] = s.p + (from + (int64_t)second * rows) * s.ld;
-                offset[i] = (uint32_t)((at * s.ld + ((lane % 8) ^ (row & 7)) * 8) * 2);
+                offset[i] = (uint32_t)((at * s.ld + contiguous_pack<packs>(row, lane % packs) * 8) * 2);
             }
         }
     }
-    // k0 .. k0 + 63 from element `from` of the side on; left: how many of them there are.
-    __device__ __forceinline__ void issue(const Side &s, int64_t from, int32_t k0, int32_t left, uint32_t buffer) const
+    // Copy i of the k from element `from` of the side on, of which there are `left`.
+    __device__ __forceinline__ void issue(int i, int64_t from, int32_t left, uint32_t buffer) const
     {
-        from += STRIDED ? k0 * s.ld : k0;
-#pragma unroll
-        for (int i = 0; i < count; i++) {
-            const uint16_t *b = base[i] + from;
-            const uint32_t at = __builtin_amdgcn_readfirstlane(to + buffer + i * THREADS * 16);
-            if (left >= kStep) {
-                copy_to_lds(at, b, offset[i]);
-            } else {
-                const uint32_t lane = threadIdx.x % 64, p = i * THREADS + threadIdx.x / 64 * 64 + lane;
-                const int32_t k = STRIDED ? p / (ROWS / 8) : ((lane % 8) ^ ((p / 8) & 7)) * 8;
-                const void *q = (const char *)b + offset[i];
-                copy_to_lds(at, k < left ? q : zeros);
-            }
+        const uint16_t *b = base[i] + from;
+        const uint32_t at = __builtin_amdgcn_readfirstlane(to + buffer + i * THREADS * 16);
+        if (left >= STEP) {
+            copy_to_lds(at, b, offset[i]);
+        } else {
+            const uint32_t lane = threadIdx.x % 64, p = i * THREADS + threadIdx.x / 64 * 64 + lane;
+            const int32_t k = STRIDED ? p / packs : contiguous_pack<STEP / 8>(p / packs, lane % packs) * 8;
+            const void *q = (const char *)b + offset[i];
+            copy_to_lds(at, k < left ? q : zeros);
         }
     }
 };
 
 // The piece of 32 rows from row0 on and 16 k from k0 on, as the matrix instruction takes it: lane l row l % 32, k 8 (l / 32) ...
-template <bool STRIDED, int ROWS>
+template <bool STRIDED, int ROWS, int STEP>
 __device__ __forceinline__ Bits8 piece(CCDC_LDS unsigned char *lds, int row0, int k0)
 {
     const uint32_t lane = threadIdx.x % 64;
@@ -132,38 +130,8 @@ __device__ __forceinline__ Bits8 piece(CCDC_LDS unsigned char *lds, int row0, in
         const Bits4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((CCDC_LDS Bits4 *)(p + 4 * ROWS * 2));
         return __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-        return *(CCDC_LDS Bits8 *)(lds + contiguous_at(row0 + lane % 32, k0 / 8 + lane / 32));
-    }
-}
-
-// Eight n of one m: n 16 half + 8 (lane / 32) ... of the piece, after the wavefront's halves have exchanged runs of four.
-__device__ __forceinline__ Eight eight_of(const Acc &c, int half)
-{
-    Eight out;
-#pragma unroll
-    for (int k = 0; k < 4; k++) {
-        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(c[8 * half + k]), __float_as_uint(c[8 * half + 4 + k]), false, false);
-        out.v[k] = __uint_as_float(r[0]);
-        out.v[4 + k] = __uint_as_float(r[1]);
-    }
-    return out;
-}
-
-// The activation of a and its derivative.
-template <class T>
-__device__ __forceinline__ void activate(int which, float a, float &value, float &slope)
-{
-    if (which == CCDC_ACT_SILU) {
-        const float e = T::planes == 1 ? __expf(-a) : expf(-a), s = 1.0f / (1.0f + e);
-        value = a * s;
-        slope = s * (1.0f + a * (1.0f - s));
-    } else if (which == CCDC_ACT_GELU) {
-        const float cdf = 0.5f * (1.0f + erff(a * 0.70710678f));
-        value = a * cdf;
-        slope = cdf + a * 0.39894228f * (T::planes == 1 ? __expf(-0.5f * a * a) : expf(-0.5f * a * a));
-    } else {
-        value = a > 0.0f ? a : a != a ? a : 0.0f;
-        slope = a > 0.0f ? 1.0f : 0.0f;
+        const uint32_t row = row0 + lane % 32;
+        return *(CCDC_LDS Bits8 *)(lds + row * (STEP * 2) + contiguous_pack<STEP / 8>(row, k0 / 8 + lane / 32) * 16);
     }
 }
 
@@ -173,7 +141,8 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
 {
     constexpr bool NS = WHAT != Product::gated && WHAT != Product::plain, MS = WHAT == Product::weight_gradient;
     constexpr bool GATED = WHAT == Product::gated;
-    constexpr int THREADS = 64 * WN * WM, TN = WN * SN * 32, TM = WM * SM * 32, BUFFER = (TN + TM) * kStep * 2;
+    constexpr int THREADS = 64 * WN * WM, TN = WN * SN * 32, TM = WM * SM * 32;
+    constexpr int STEP = 64, BUFFER = (TN + TM) * STEP * 2;
     __shared__ __attribute__((aligned(1024))) unsigned char memory[2 * BUFFER];
     CCDC_LDS unsigned char *lds = (CCDC_LDS unsigned char *)memory;
     const uint32_t lds_at = (uint32_t)(uintptr_t)lds;
@@ -196,10 +165,10 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
         sn.p += from * sn.ld;
         sm.p += from * sm.ld + half * sm.segment;
     }
-    Copies<NS, TN, THREADS> cn;
-    Copies<MS, TM, THREADS> cm;
+    Copies<NS, TN, THREADS, STEP> cn;
+    Copies<MS, TM, THREADS, STEP> cm;
     cn.template set<GATED>(sn, tile_n, a.rows_n, lds_at);
-    cm.template set<false>(sm, tile_m, a.rows_m, lds_at + TN * kStep * 2);
+    cm.template set<false>(sm, tile_m, a.rows_m, lds_at + TN * STEP * 2);
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wn = wave % WN * SN * 32, wm = wave / WN * SM * 32;
@@ -212,59 +181,186 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0.0f;
 
     // steps: planes of either side, then ranges of k, then k
-    const int32_t in_k = (K + kStep - 1) / kStep, steps = in_k * a.segments * (T::planes == 1 ? 1 : 6);
-    int32_t next_k = 0, next_segment = 0, next_planes = 0;
-    const auto issue = [&](uint32_t buffer) {
-        int64_t from_n = next_segment ? sn.segment : 0, from_m = next_segment ? sm.segment : 0;
-        if constexpr (T::planes == 3) {           // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
-            const int pn = (0x001102 >> (4 * next_planes)) & 15, pm = (0x010120 >> (4 * next_planes)) & 15;
-            from_n += pn * sn.plane;
-            from_m += pm * sm.plane;
-        }
-        const int32_t k0 = next_k * kStep, left = K - k0;
-        cn.issue(sn, from_n, k0, left, buffer);
-        cm.issue(sm, from_m, k0, left, buffer);
-        if (++next_k == in_k) {
-            next_k = 0;
-            if (++next_segment == a.segments) next_segment = 0, next_planes++;
+    const int32_t in_k = (K + STEP - 1) / STEP, steps = in_k * a.segments * (T::planes == 1 ? 1 : 6);
+    // What is copied next of a side: its place in the side's order of steps.
+    struct Next {
+        int32_t k = 0, segment = 0, planes = 0;
+    };
+    Next next_n, next_m;
+    const auto copies = [&](const auto &side, const Side &s, Next &at, bool of_n, uint32_t buffer) {
+        constexpr bool strided = std::decay_t<decltype(side)>::strided;
+        int64_t from = at.segment ? s.segment : 0;
+        if constexpr (T::planes == 3)             // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+            from += (((of_n ? 0x001102 : 0x010120) >> (4 * at.planes)) & 15) * s.plane;
+        const int64_t k0 = (int64_t)at.k * STEP;
+        from += strided ? k0 * s.ld : k0;
+#pragma unroll
+        for (int i = 0; i < std::decay_t<decltype(side)>::count; i++) side.issue(i, from, K - (int32_t)k0, buffer);
+        if (++at.k == in_k) {
+            at.k = 0;
+            if (++at.segment == a.segments) at.segment = 0, at.planes++;
         }
     };
+    const auto copy_n = [&](int32_t s) { copies(cn, sn, next_n, true, s % 2 * BUFFER); };
+    const auto copy_m = [&](int32_t s) { copies(cm, sm, next_m, false, s % 2 * BUFFER); };
 
-    if (steps > 0) issue(0);
-    for (int32_t s = 0; s < steps; s++) {
-        // this step's copies are there, and every wavefront has read the step before it
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (s + 1 < steps) issue((s + 1) % 2 * BUFFER);
-        CCDC_LDS unsigned char *n = lds + s % 2 * BUFFER, *m = n + TN * kStep * 2;
-#pragma unroll
-        for (int k = 0; k < kStep; k += 16) {
-            Bits8 pn[SN], pm[SM];
-#pragma unroll
-            for (int i = 0; i < SN; i++) pn[i] = piece<NS, TN>(n, wn + i * 32, k);
-#pragma unroll
-            for (int j = 0; j < SM; j++) pm[j] = piece<MS, TM>(m, wm + j * 32, k);
-#pragma unroll
-            for (int i = 0; i < SN; i++)
-#pragma unroll
-                for (int j = 0; j < SM; j++) acc[i][j] = multiply<T>(pn[i], pm[j], acc[i][j]);
+    const auto piece_n = [&](int32_t s, int i, int k) { return piece<NS, TN, STEP>(lds + s % 2 * BUFFER, wn + i * 32, k); };
+    const auto piece_m = [&](int32_t s, int j, int k) { return piece<MS, TM, STEP>(lds + s % 2 * BUFFER + TN * STEP * 2, wm + j * 32, k); };
+    const auto meet = [] {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto reads_there = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+    // and copies, but those of side N that were begun last
+    const auto all_there = [](bool but_n) {
+        if (but_n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(cn)::count) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    };
+    if constexpr (THREADS == 512) {
+        // Two wavefronts a SIMD, the second of each a phase behind: while one reads pieces, the other multiplies its own, and
+        // they change over at a barrier.  A wavefront has two turns a step: it reads all its pieces of side N and half
+        // of side M, then the other half.  So N is free for the step after the next when the second of the two has had its first
+        // turn, and M with the step: the copies are begun half in each turn, three to six phases before the barrier at
+        // which they are waited for.
+        constexpr int H = SM / 2, KS = STEP / 16;
+        const bool second = wave >= 4;
+        if (steps > 0) {
+            copy_n(0);
+            copy_m(0);
+            if (steps > 1) copy_n(1);
+            all_there(steps > 1);
+            meet();
         }
+        if (second) meet();
+        for (int32_t s = 0; s < steps; s++) {
+            Bits8 pn[KS][SN], pm[KS][H];
+#pragma unroll
+            for (int turn = 0; turn < 2; turn++) {
+#pragma unroll
+                for (int k = 0; k < KS; k++) {
+#pragma unroll
+                    for (int i = 0; i < SN; i++)
+                        if (turn == 0) pn[k][i] = piece_n(s, i, k * 16);
+#pragma unroll
+                    for (int j = 0; j < H; j++) pm[k][j] = piece_m(s, turn * H + j, k * 16);
+                }
+                if (turn == 0 && s + 1 < steps) copy_m(s + 1);
+                if (turn == 1 && s + 2 < steps) copy_n(s);
+                if (turn == 1 && second) all_there(s + 2 < steps);
+                else reads_there();
+                meet();
+                __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                for (int k = 0; k < KS; k++)
+#pragma unroll
+                    for (int i = 0; i < SN; i++)
+#pragma unroll
+                        for (int j = 0; j < H; j++) acc[i][turn * H + j] = multiply<T>(pn[k][i], pm[k][j], acc[i][turn * H + j]);
+                __builtin_amdgcn_s_setprio(0);
+                if (turn == 1 && !second) all_there(s + 2 < steps);
+                meet();
+            }
+        }
+        if (!second) meet();
+    } else {
+        // One wavefront a SIMD, two workgroups a CU.  The pieces of the next 16 k are read while these are multiplied, the
+        // first of a step during the last of the step before: by then its copies are waited for, and with that barrier every
+        // wavefront has read all of the buffer, which the step after it is copied to.
+        Bits8 pn[2][SN], pm[2][SM];
+        const auto read = [&](int to, int32_t s, int k) {
+#pragma unroll
+            for (int i = 0; i < SN; i++) pn[to][i] = piece_n(s, i, k);
+#pragma unroll
+            for (int j = 0; j < SM; j++) pm[to][j] = piece_m(s, j, k);
+        };
+        const auto copy = [&](int32_t s) {
+            copy_n(s);
+            copy_m(s);
+        };
+        if (steps > 0) {
+            copy(0);
+            all_there(false);
+            meet();
+            if (steps > 1) copy(1);
+            read(0, 0, 0);
+        }
+        for (int32_t s = 0; s < steps; s++) {
+#pragma unroll
+            for (int k = 0; k < STEP / 16; k++) {
+                if (k + 1 < STEP / 16) {
+                    read((k + 1) % 2, s, (k + 1) * 16);
+                } else if (s + 1 < steps) {
+                    all_there(false);
+                    meet();
+                    if (s + 2 < steps) copy(s);
+                    read(0, s + 1, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);       // left to itself the compiler puts the reads after the products
+#pragma unroll
+                for (int i = 0; i < SN; i++)
+#pragma unroll
+                    for (int j = 0; j < SM; j++) acc[i][j] = multiply<T>(pn[k % 2][i], pm[k % 2][j], acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        meet();
     }
 
+    // The result goes through LDS, a wavefront's rows of 64 n at a time, each by itself: an accumulator's lanes have four n of 32 rows,
+    // a store of which would be 32 pieces of as many lines; after it eight lanes have a row's 64.
+    static_assert(SN == 2);
+    using E = typename T::elem;
+    constexpr bool NARROW = sizeof(E) == 2 && WHAT != Product::gated && WHAT != Product::gated_gradient;      // staged as stored
 #pragma unroll
     for (int j = 0; j < SM; j++) {
-        const int32_t m = tile_m + wm + j * 32 + lane % 32;
-        const bool row_there = m < a.rows_m;
-        RowOf of{};
-        if (GATED && a.drop.threshold && row_there) of = a.row_of[m];
+        CCDC_LDS unsigned char *stage = lds + (wave * 2 + j % 2) * 8192;
 #pragma unroll
-        for (int half_n = 0; half_n < 2; half_n++) {
+        for (int i = 0; i < SN; i++)
+#pragma unroll
+            for (int g = 0; g < 4; g++) {
+                const uint32_t row = lane % 32, four = i * 8 + g * 2 + lane / 32;
+                if constexpr (NARROW) {
+                    typedef E Four __attribute__((ext_vector_type(4)));
+                    Four v;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) v[e] = T::narrow(acc[i][j][4 * g + e]);
+                    *(CCDC_LDS Four *)(stage + row * 128 + (four / 2 ^ row / 2 % 8) * 16 + four % 2 * 8) = v;
+                } else {
+                    typedef float Four __attribute__((ext_vector_type(4)));
+                    Four v;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) v[e] = acc[i][j][4 * g + e];
+                    *(CCDC_LDS Four *)(stage + row * 256 + (four ^ row % 16) * 16) = v;
+                }
+            }
+        // numbers 8 pack ... 8 pack + 7 of a row
+        const auto staged = [&](uint32_t row, uint32_t pack) {
+            typedef float Four __attribute__((ext_vector_type(4)));
+            Eight v;
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                const Four f = *(CCDC_LDS Four *)(stage + row * 256 + ((pack * 2 + h) ^ row % 16) * 16);
+#pragma unroll
+                for (int e = 0; e < 4; e++) v.v[4 * h + e] = f[e];
+            }
+            return v;
+        };
+        constexpr int LANES = GATED ? 4 : 8;              // that have a row: 32 of a and of u, or 64
+#pragma unroll
+        for (int q = 0; q < 32 * LANES / 64; q++) {
+            const uint32_t row = q * (64 / LANES) + lane / LANES, pack = lane % LANES;
+            const int32_t m = tile_m + wm + j * 32 + row;
+            if (m >= a.rows_m) continue;
             if constexpr (GATED) {
-                static_assert(!GATED || SN == 2);
-                const int32_t f = tile_n + wn / 2 + half_n * 16 + lane / 32 * 8;
-                const Eight va = eight_of(acc[0][j], half_n), vu = eight_of(acc[1][j], half_n);
-                if (!row_there || f >= a.ldh) continue;
+                const int32_t f = tile_n + wn / 2 + pack * 8;
+                if (f >= a.ldh) continue;
+                const Eight va = staged(row, pack), vu = staged(row, 4 + pack);
                 Eight h, P, Q, keep;
-                if (a.drop.threshold) keep = dropout_factors(a.drop, of.id, of.token, f / 8);
+                if (a.drop.threshold) {
+                    const RowOf of = a.row_of[m];
+                    keep = dropout_factors(a.drop, of.id, of.token, f / 8);
+                }
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     float value, slope;
@@ -280,27 +376,36 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
                     store_eight<ElemF32>(a.Q + at, Q, 8);
                 }
             } else {
+                const int32_t n = tile_n + wn + pack * 8;
+                if constexpr (WHAT == Product::gated_gradient) {
+                    if (n >= a.ldh) continue;
+                    const Eight v = staged(row, pack);
+                    const int64_t at = (int64_t)m * a.ldh + n;
+                    const Eight P = load_eight<ElemF32>(a.P + at, 8), Q = load_eight<ElemF32>(a.Q + at, 8);
+                    Eight da, du;
 #pragma unroll
-                for (int i = 0; i < SN; i++) {
-                    const int32_t n = tile_n + wn + i * 32 + half_n * 16 + lane / 32 * 8;
-                    Eight v = eight_of(acc[i][j], half_n);
-                    if constexpr (WHAT == Product::gated_gradient) {
-                        if (!row_there || n >= a.ldh) continue;
-                        const int64_t at = (int64_t)m * a.ldh + n;
-                        const Eight P = load_eight<ElemF32>(a.P + at, 8), Q = load_eight<ElemF32>(a.Q + at, 8);
-                        Eight da, du;
+                    for (int e = 0; e < 8; e++) {
+                        da.v[e] = v.v[e] * P.v[e], du.v[e] = v.v[e] * Q.v[e];
+                        if (n + e >= a.rows_n) da.v[e] = du.v[e] = 0.0f;
+                    }
+                    uint16_t *to = a.h + (int64_t)m * 2 * a.ldh + n;
+                    store_side<T>(to, a.plane_h, da);
+                    store_side<T>(to + a.second_h, a.plane_h, du);
+                } else {
+                    if (n >= a.rows_n) continue;
+                    E *to = (E *)a.c + file * a.file_c + half * a.half_c + (int64_t)m * a.ldc + n;
+                    if constexpr (NARROW) {
+                        const Bits8 v = *(CCDC_LDS Bits8 *)(stage + row * 128 + (pack ^ row / 2 % 8) * 16);
+                        const int valid = fresh(a.rows_n - n);
+                        if (valid >= 8) {
+                            store_any<Bits8, E>(to, v);
+                        } else {
 #pragma unroll
-                        for (int e = 0; e < 8; e++) {
-                            da.v[e] = v.v[e] * P.v[e], du.v[e] = v.v[e] * Q.v[e];
-                            if (n + e >= a.rows_n) da.v[e] = du.v[e] = 0.0f;
+                            for (int e = 0; e < 8; e++)
+                                if (e < valid) to[e] = (E)v[e];
                         }
-                        uint16_t *to = a.h + (int64_t)m * 2 * a.ldh + n;
-                        store_side<T>(to, a.plane_h, da);
-                        store_side<T>(to + a.second_h, a.plane_h, du);
                     } else {
-                        if (!row_there || n >= a.rows_n) continue;
-                        typename T::elem *to = (typename T::elem *)a.c + file * a.file_c + half * a.half_c + (int64_t)m * a.ldc + n;
-                        store_eight<T>(to, v, a.rows_n - n);
+                        store_eight<T>(to, staged(row, pack), a.rows_n - n);
                     }
                 }
             }

@@ -76,6 +76,29 @@ __device__ __forceinline__ void store_side(uint16_t *p, int64_t plane, const Eig
     }
 }
 
+// The activation of a and its derivative.
+template <class T>
+__device__ __forceinline__ void activate(int which, float a, float &value, float &slope)
+{
+    if (which == CCDC_ACT_SILU) {
+        const float e = T::planes == 1 ? __expf(-a) : expf(-a), s = 1.0f / (1.0f + e);
+        value = a * s;
+        slope = s * (1.0f + a * (1.0f - s));
+    } else if (which == CCDC_ACT_GELU) {
+        const float cdf = 0.5f * (1.0f + erff(a * 0.70710678f));
+        value = a * cdf;
+        slope = cdf + a * 0.39894228f * (T::planes == 1 ? __expf(-0.5f * a * a) : expf(-0.5f * a * a));
+    } else {
+        value = a > 0.0f ? a : a != a ? a : 0.0f;
+        slope = a > 0.0f ? 1.0f : 0.0f;
+    }
+}
+
+// The forward for at most kFewRows rows (few.hip).
+constexpr int64_t kFewRows = 64;
+int few_forward(const ccdc_block_t *b, int64_t rows, const void *x, int64_t ldx, const void *W_in, const void *W_out, void *y, int64_t ldy,
+                void *h, const Dropout &drop, hipStream_t st);
+
 // The bytes of a workspace or of what is saved from `at` on.
 template <class E = void>
 inline E *inside_of(const void *base, size_t at)
