@@ -41,11 +41,12 @@ __device__ __forceinline__ Loaded<T> load_k(const typename T::elem *p)
 
 // The same where a row may end: zeros past it.
 template <class T>
-__device__ __forceinline__ Loaded<T> load_k(const typename T::elem *p, int left)
+__device__ __forceinline__ Loaded<T> load_end(const typename T::elem *p, int left)
 {
     constexpr int W = 16 / sizeof(typename T::elem);
-    Loaded<T> v;
     left = fresh(left);
+    if (left >= 8) return load_k<T>(p);
+    Loaded<T> v;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         const typename T::elem e = p[min(i, left - 1)];      // the row's last element where it has ended
@@ -102,7 +103,7 @@ template <class T, bool GATED, int S, int MT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_few(const FewArgs a)
 {
     using E = typename T::elem;
-    constexpr int R = 16 / S, STREAMS = GATED ? 2 : 1, STEP = 32 * S, COLUMNS = MT * 16 / S, AHEAD = T::planes == 3 || MT > 2 ? 2 : 4;
+    constexpr int R = 16 / S, STREAMS = GATED ? 2 : 1, STEP = 32 * S, COLUMNS = MT * 16 / S, AHEAD = T::planes == 3 ? (MT > 2 ? 1 : 2) : MT > 1 ? 2 : 4;
     static_assert(S == 1 || MT == 1);
     __shared__ float sums[WAVES][STREAMS][MT][16][17];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16;
@@ -116,43 +117,43 @@ __global__ __launch_bounds__(64 * WAVES) void k_few(const FewArgs a)
 
     Acc4 acc[STREAMS][MT] = {};
     const int32_t whole = a.K / STEP;
-    int32_t s = wave;
-    for (; s + (AHEAD - 1) * WAVES < whole; s += AHEAD * WAVES) {
+    const auto add = [&](const Loaded<T> (&lw)[STREAMS], const Loaded<T> (&lx)[MT]) {
+        Operand<T> ox[MT];
+#pragma unroll
+        for (int t = 0; t < MT; t++) ox[t] = operand<T>(lx[t]);
+#pragma unroll
+        for (int i = 0; i < STREAMS; i++) {
+            const Operand<T> ow = operand<T>(lw[i]);
+#pragma unroll
+            for (int t = 0; t < MT; t++) acc[i][t] = multiply<T>(ow, ox[t], acc[i][t]);
+        }
+    };
+    // The step that the rows end in is one wavefront's, asked for before its whole ones and added after them.
+    const bool last = a.K % STEP && whole % WAVES == wave;
+    Loaded<T> ew[STREAMS], ex[MT];
+    if (last) {
+        const int64_t k = (int64_t)whole * STEP;
+        const int left = a.K - (int)k - offset;
+#pragma unroll
+        for (int i = 0; i < STREAMS; i++) ew[i] = load_end<T>(w[i] + k, left);
+#pragma unroll
+        for (int t = 0; t < MT; t++) ex[t] = load_end<T>(x[t] + k, left);
+    }
+    for (int32_t s = wave; s < whole; s += AHEAD * WAVES) {
         Loaded<T> lw[AHEAD][STREAMS], lx[AHEAD][MT];
 #pragma unroll
         for (int u = 0; u < AHEAD; u++) {
-            const int64_t k = (int64_t)(s + u * WAVES) * STEP;
+            const int64_t k = (int64_t)min(s + u * WAVES, whole - 1) * STEP;      // past the wavefront's steps: not added
 #pragma unroll
             for (int i = 0; i < STREAMS; i++) lw[u][i] = load_k<T>(w[i] + k);
 #pragma unroll
             for (int t = 0; t < MT; t++) lx[u][t] = load_k<T>(x[t] + k);
         }
 #pragma unroll
-        for (int u = 0; u < AHEAD; u++) {
-            Operand<T> ox[MT];
-#pragma unroll
-            for (int t = 0; t < MT; t++) ox[t] = operand<T>(lx[u][t]);
-#pragma unroll
-            for (int i = 0; i < STREAMS; i++) {
-                const Operand<T> ow = operand<T>(lw[u][i]);
-#pragma unroll
-                for (int t = 0; t < MT; t++) acc[i][t] = multiply<T>(ow, ox[t], acc[i][t]);
-            }
-        }
+        for (int u = 0; u < AHEAD; u++)
+            if (s + u * WAVES < whole) add(lw[u], lx[u]);
     }
-    for (; s * (int64_t)STEP < a.K; s += WAVES) {
-        const int64_t k = (int64_t)s * STEP;
-        const int left = a.K - (int)k - offset;
-        Operand<T> ow[STREAMS];
-#pragma unroll
-        for (int i = 0; i < STREAMS; i++) ow[i] = operand<T>(left >= 8 ? load_k<T>(w[i] + k) : load_k<T>(w[i] + k, left));
-#pragma unroll
-        for (int t = 0; t < MT; t++) {
-            const Operand<T> ox = operand<T>(left >= 8 ? load_k<T>(x[t] + k) : load_k<T>(x[t] + k, left));
-#pragma unroll
-            for (int i = 0; i < STREAMS; i++) acc[i][t] = multiply<T>(ow[i], ox, acc[i][t]);
-        }
-    }
+    if (last) add(ew, ex);
 
     // lane l has rows 4 (l / 16) ... of column l % 16
 #pragma unroll

@@ -7,6 +7,9 @@ namespace {
 using namespace ccdc;
 
 constexpr int kJoinWaves = 4;         // wavefronts of a workgroup where a row has fewer
+// Rows that a workgroup of the gradient has at a time.  A row is a chain of four sums over it and three waits for memory, 9 us of them
+// at 2048 columns, so a chunk's rows go several abreast: 14336 x 2048 bf16 one at a time 298 us.
+constexpr int teams(int waves) { return waves <= 2 ? 4 : waves == 4 ? 2 : 1; }
 
 struct JoinArgs {
     const void *x, *f, *w_post, *gate, *w_pre;    // forward; backward: x is dr
@@ -21,50 +24,42 @@ struct JoinArgs {
     Dropout drop;
 };
 
-// The sum of a value over the threads of a row: a wavefront by exchanges in a tree, wavefronts by LDS in their order.
+// Sums over the threads of a row: a wavefront by exchanges in a tree, wavefronts by LDS in their order.  Two halves of the LDS in
+// turn, so that one barrier a sum is enough: who writes the first half again has met the others since they read it.
 template <int WAVES>
-__device__ __forceinline__ float row_sum(float v, float *part)
-{
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    if constexpr (WAVES > 1) {
-        const int wave = threadIdx.x / 64;
-        __syncthreads();                          // the last sum has been read
-        if (threadIdx.x % 64 == 0) part[wave] = v;
-        __syncthreads();
-        v = part[0];
-#pragma unroll
-        for (int i = 1; i < WAVES; i++) v += part[i];
-    }
-    return v;
-}
+struct RowSums {
+    float *part;                                  // [2][2 * WAVES] of the row
+    int at = 0;
 
-// Two sums at once.
-template <int WAVES>
-__device__ __forceinline__ void row_sums(float &a, float &b, float *part)
-{
+    template <int COUNT>
+    __device__ __forceinline__ void add(float (&v)[COUNT])
+    {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) {
-        a += __shfl_xor(a, off, 64);
-        b += __shfl_xor(b, off, 64);
-    }
-    if constexpr (WAVES > 1) {
-        const int wave = threadIdx.x / 64;
-        __syncthreads();
-        if (threadIdx.x % 64 == 0) {
-            part[2 * wave] = a;
-            part[2 * wave + 1] = b;
-        }
-        __syncthreads();
-        a = part[0];
-        b = part[1];
+        for (int off = 32; off > 0; off >>= 1)
 #pragma unroll
-        for (int i = 1; i < WAVES; i++) {
-            a += part[2 * i];
-            b += part[2 * i + 1];
+            for (int c = 0; c < COUNT; c++) v[c] += __shfl_xor(v[c], off, 64);
+        if constexpr (WAVES > 1) {
+            float *slot = part + at;
+            at = 2 * WAVES - at;
+            if (fresh(threadIdx.x) % 64 == 0)
+#pragma unroll
+                for (int c = 0; c < COUNT; c++) slot[threadIdx.x / 64 % WAVES * COUNT + c] = v[c];
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < COUNT; c++) v[c] = slot[c];
+#pragma unroll
+            for (int i = 1; i < WAVES; i++)
+#pragma unroll
+                for (int c = 0; c < COUNT; c++) v[c] += slot[i * COUNT + c];
         }
     }
-}
+    __device__ __forceinline__ float add(float v)
+    {
+        float one[1] = {v};
+        add(one);
+        return one[0];
+    }
+};
 
 // What a thread holds of a row: packs (threadIdx in the row) + i * (threads of the row).
 template <int WAVES, int PACKS>
@@ -81,7 +76,7 @@ __device__ __forceinline__ int pack_of(int i)
 // v becomes v hat = (v - mean, where centred) * rstd; returns rstd.  Statistics of the held row: the mean first, then
 // the squares of what is left, as the formula says (no difference of large sums).
 template <bool CENTRED, int WAVES, int PACKS>
-__device__ __forceinline__ float normalise(Share<WAVES, PACKS> &v, int width, float eps, float *part)
+__device__ __forceinline__ float normalise(Share<WAVES, PACKS> &v, int width, float eps, RowSums<WAVES> &sums)
 {
     if constexpr (CENTRED) {
         float sum = 0.0f;
@@ -89,7 +84,7 @@ __device__ __forceinline__ float normalise(Share<WAVES, PACKS> &v, int width, fl
         for (int i = 0; i < PACKS; i++)
 #pragma unroll
             for (int e = 0; e < 8; e++) sum += v.p[i].v[e];          // past the row's end: zeros
-        const float mean = row_sum<WAVES>(sum, part) / (float)width;
+        const float mean = sums.add(sum) / (float)width;
 #pragma unroll
         for (int i = 0; i < PACKS; i++) {
             const int valid = fresh(width - pack_of<WAVES>(i) * 8);
@@ -103,7 +98,7 @@ __device__ __forceinline__ float normalise(Share<WAVES, PACKS> &v, int width, fl
     for (int i = 0; i < PACKS; i++)
 #pragma unroll
         for (int e = 0; e < 8; e++) square += v.p[i].v[e] * v.p[i].v[e];
-    const float rstd = 1.0f / sqrtf(row_sum<WAVES>(square, part) / (float)width + eps);
+    const float rstd = 1.0f / sqrtf(sums.add(square) / (float)width + eps);
 #pragma unroll
     for (int i = 0; i < PACKS; i++)
 #pragma unroll
@@ -114,7 +109,7 @@ __device__ __forceinline__ float normalise(Share<WAVES, PACKS> &v, int width, fl
 // e becomes the gradient of v from that of v hat: rstd (e - v hat mean(e v hat) [- mean(e)]).
 template <bool CENTRED, int WAVES, int PACKS>
 __device__ __forceinline__ void norm_gradient(Share<WAVES, PACKS> &e, const Share<WAVES, PACKS> &hat, float rstd, int width,
-                                              float *part)
+                                              RowSums<WAVES> &sums)
 {
     float dot = 0.0f, sum = 0.0f;
 #pragma unroll
@@ -124,8 +119,13 @@ __device__ __forceinline__ void norm_gradient(Share<WAVES, PACKS> &e, const Shar
             dot += e.p[i].v[k] * hat.p[i].v[k];
             if constexpr (CENTRED) sum += e.p[i].v[k];
         }
-    if constexpr (CENTRED) row_sums<WAVES>(dot, sum, part);
-    else dot = row_sum<WAVES>(dot, part);
+    if constexpr (CENTRED) {
+        float both[2] = {dot, sum};
+        sums.add(both);
+        dot = both[0], sum = both[1];
+    } else {
+        dot = sums.add(dot);
+    }
     dot /= (float)width;
     sum /= (float)width;
 #pragma unroll
@@ -146,7 +146,7 @@ __device__ __forceinline__ Share<WAVES, PACKS> load_row(const void *base, int64_
     Share<WAVES, PACKS> s;
 #pragma unroll
     for (int i = 0; i < PACKS; i++) {
-        const int c = pack_of<WAVES>(i) * 8;
+        const int c = fresh(pack_of<WAVES>(i) * 8);
         if (c < width) s.p[i] = load_eight<T, !STREAM>((const typename T::elem *)base + at + c, width - c);
         else s.p[i] = {};
     }
@@ -158,7 +158,7 @@ __device__ __forceinline__ void store_row(void *base, int64_t at, int width, con
 {
 #pragma unroll
     for (int i = 0; i < PACKS; i++) {
-        const int c = pack_of<WAVES>(i) * 8;
+        const int c = fresh(pack_of<WAVES>(i) * 8);
         if (c < width) store_eight<T>((typename T::elem *)base + at + c, s.p[i], width - c);
     }
 }
@@ -194,7 +194,8 @@ __device__ __forceinline__ void drop(Share<WAVES, PACKS> &v, const Dropout &d, c
 template <class T, bool CENTRED, int WAVES, int PACKS>
 __global__ __launch_bounds__(64 * (WAVES > 1 ? WAVES : kJoinWaves)) void k_join(const JoinArgs a)
 {
-    __shared__ float part[WAVES > 1 ? 2 * WAVES : 1];
+    __shared__ float part[WAVES > 1 ? 4 * WAVES : 1];
+    RowSums<WAVES> sums{part};
     const int row = WAVES > 1 ? (int)blockIdx.x : (int)(blockIdx.x * kJoinWaves + threadIdx.x / 64);
     if (row >= a.rows) return;
     const int64_t at = row * a.ld;
@@ -202,7 +203,7 @@ __global__ __launch_bounds__(64 * (WAVES > 1 ? WAVES : kJoinWaves)) void k_join(
     if (a.f) {
         Share<WAVES, PACKS> z = load_row<T, WAVES, PACKS>(a.f, at, a.width);
         const RowOf of = a.row_of[row];
-        normalise<CENTRED>(z, a.width, a.eps, part);
+        normalise<CENTRED>(z, a.width, a.eps, sums);
         times<T>(z, a.w_post, 0, a.width);
         times<T>(z, a.gate, of.file * a.ld_gate, a.width);
         drop(z, a.drop, of, a.width);
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(64 * (WAVES > 1 ? WAVES : kJoinWaves)) void k_join(
     }
     if (a.y) store_row<T>(a.y, at, a.width, y);
     if (a.n) {
-        normalise<CENTRED>(y, a.width, a.eps, part);
+        normalise<CENTRED>(y, a.width, a.eps, sums);
         times<T>(y, a.w_pre, 0, a.width);
         store_row<T>(a.n, at, a.width, y);
     }
@@ -228,13 +229,15 @@ __global__ __launch_bounds__(64 * (WAVES > 1 ? WAVES : kJoinWaves)) void k_join(
 // all three gradients: with S = sum D(dy) fhat, dw_post = gate S and dgate = w_post S; dw_pre = sum dn yhat.  A thread keeps its
 // columns' sums over the chunk's rows in registers; k_learned adds the chunks.
 template <class T, bool CENTRED, int WAVES, int PACKS>
-__global__ __launch_bounds__(64 * (WAVES > 1 ? WAVES : kJoinWaves)) void k_join_gradient(const JoinArgs a)
+__global__ __launch_bounds__(64 * WAVES * teams(WAVES)) void k_join_gradient(const JoinArgs a)
 {
-    __shared__ float part[WAVES > 1 ? 2 * WAVES : 1];
-    __shared__ float add[WAVES > 1 ? 1 : kJoinWaves * 64 * 8];
     using E = typename T::elem;
+    constexpr int TEAMS = teams(WAVES), ROW = 64 * WAVES;     // rows at a time, threads of a row
+    __shared__ float part[TEAMS][WAVES > 1 ? 4 * WAVES : 1];
+    __shared__ float add[TEAMS > 1 ? TEAMS * ROW * 8 : 1];
     const Chunk chunk = a.chunks[blockIdx.x];
-    const int step = WAVES > 1 ? 1 : kJoinWaves, start = WAVES > 1 ? 0 : (int)threadIdx.x / 64;
+    const int team = __builtin_amdgcn_readfirstlane(threadIdx.x / ROW);
+    RowSums<WAVES> sums{part[team]};
     // a workgroup of sixteen wavefronts has 128 registers a lane: its sums are in LDS, each lane's its own
     constexpr bool in_lds = WAVES == 16;
     __shared__ float lds_sum[in_lds ? 2 * PACKS * 8 * 64 * WAVES : 1];
@@ -245,22 +248,26 @@ __global__ __launch_bounds__(64 * (WAVES > 1 ? WAVES : kJoinWaves)) void k_join_
     };
     if constexpr (in_lds)
         for (int i = 0; i < 2 * PACKS * 8; i++) lds_sum[i * (64 * WAVES) + threadIdx.x] = 0.0f;
-    for (int r = start; r < chunk.rows; r += step) {
-        const int64_t row = chunk.first + r, at = row * a.ld;
-        // the parameters are asked for again in every row: kept over the rows they are the registers of other wavefronts
-        const int width = fresh_uniform(a.width);
-        const void *w_post = fresh_uniform(a.w_post), *w_pre = fresh_uniform(a.w_pre);
+    const auto *args = (const __attribute__((address_space(4))) JoinArgs *)__builtin_amdgcn_kernarg_segment_ptr();
+    for (int r = team; r - team < chunk.rows; r += TEAMS) {
+        const bool own = r < chunk.rows;          // else with the others to the barriers, on the last row
+        // The arguments, and the parameters that they point to, are asked for again in every row: kept over the rows they are more
+        // scalar registers than there are, and the vector registers of other wavefronts.
+        const auto &a = *fresh_uniform(args);
+        const int width = a.width;
+        const int64_t row = chunk.first + (own ? r : chunk.rows - 1), at = row * a.ld;
         Share<WAVES, PACKS> dy = {};
         if (a.dn) {
             dy = load_row<T, WAVES, PACKS>(a.dn, at, width);
             Share<WAVES, PACKS> hat = load_row<T, WAVES, PACKS>(a.y_in, at, width);
-            const float rstd = normalise<CENTRED>(hat, width, a.eps, part);
+            const float rstd = normalise<CENTRED>(hat, width, a.eps, sums);
+            if (own)
 #pragma unroll
-            for (int i = 0; i < PACKS; i++)
+                for (int i = 0; i < PACKS; i++)
 #pragma unroll
-                for (int k = 0; k < 8; k++) sum_at(1, i, k) += dy.p[i].v[k] * hat.p[i].v[k];
-            times<T>(dy, w_pre, 0, width);
-            norm_gradient<CENTRED>(dy, hat, rstd, width, part);
+                    for (int k = 0; k < 8; k++) sum_at(1, i, k) += dy.p[i].v[k] * hat.p[i].v[k];
+            times<T>(dy, a.w_pre, 0, width);
+            norm_gradient<CENTRED>(dy, hat, rstd, width, sums);
         }
         if (a.x) {
             const Share<WAVES, PACKS> dr = load_row<T, WAVES, PACKS>(a.x, at, width);
@@ -269,10 +276,10 @@ __global__ __launch_bounds__(64 * (WAVES > 1 ? WAVES : kJoinWaves)) void k_join_
 #pragma unroll
                 for (int k = 0; k < 8; k++) dy.p[i].v[k] += dr.p[i].v[k];
         }
-        if (a.y) {
+        if (a.y && own) {
 #pragma unroll
             for (int i = 0; i < PACKS; i++) {
-                const int c = pack_of<WAVES>(i) * 8;
+                const int c = fresh(pack_of<WAVES>(i) * 8);
                 if (c >= width) continue;
                 Eight dx;
 #pragma unroll
@@ -283,22 +290,24 @@ __global__ __launch_bounds__(64 * (WAVES > 1 ? WAVES : kJoinWaves)) void k_join_
         if (a.f) {
             Share<WAVES, PACKS> hat = load_row<T, WAVES, PACKS>(a.f, at, width);
             const RowOf of = a.row_of[row];
-            const float rstd = normalise<CENTRED>(hat, width, a.eps, part);
+            const Dropout drop{{a.drop.key[0], a.drop.key[1]}, a.drop.site, a.drop.threshold, a.drop.scale};
+            const float rstd = normalise<CENTRED>(hat, width, a.eps, sums);
 #pragma unroll
             for (int i = 0; i < PACKS; i++) {
-                const int unit = pack_of<WAVES>(i);
-                if (a.drop.threshold && unit * 8 < width) {
-                    const Eight f = dropout_factors(a.drop, of.id, of.token, unit);
+                const int unit = fresh(pack_of<WAVES>(i));
+                if (drop.threshold && unit * 8 < width) {
+                    const Eight f = dropout_factors(drop, of.id, of.token, unit);
 #pragma unroll
                     for (int k = 0; k < 8; k++) dy.p[i].v[k] = kept(dy.p[i].v[k], f.v[k]);
                 }
+                if (own)
 #pragma unroll
-                for (int k = 0; k < 8; k++) sum_at(0, i, k) += dy.p[i].v[k] * hat.p[i].v[k];
+                    for (int k = 0; k < 8; k++) sum_at(0, i, k) += dy.p[i].v[k] * hat.p[i].v[k];
             }
-            times<T>(dy, w_post, 0, width);
+            times<T>(dy, a.w_post, 0, width);
             times<T>(dy, a.gate, of.file * a.ld_gate, width);
-            norm_gradient<CENTRED>(dy, hat, rstd, width, part);
-            if (a.n) store_row<T>(a.n, at, width, dy);
+            norm_gradient<CENTRED>(dy, hat, rstd, width, sums);
+            if (a.n && own) store_row<T>(a.n, at, width, dy);
         }
     }
     if (!a.sums) return;
@@ -307,22 +316,22 @@ __global__ __launch_bounds__(64 * (WAVES > 1 ? WAVES : kJoinWaves)) void k_join_
     for (int s = 0; s < 2; s++)
 #pragma unroll
         for (int i = 0; i < PACKS; i++) {
-            const int c = pack_of<WAVES>(i) * 8;
+            const int c = fresh(pack_of<WAVES>(i) * 8);
             Eight v;
 #pragma unroll
             for (int k = 0; k < 8; k++) v.v[k] = sum_at(s, i, k);
-            if constexpr (WAVES == 1) {           // the workgroup's wavefronts have the same columns: added in their order
-                const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+            if constexpr (TEAMS > 1) {            // all teams have the same columns: added in their order
+                const int in_row = threadIdx.x % ROW;
 #pragma unroll
-                for (int k = 0; k < 8; k++) add[(wave * 8 + k) * 64 + lane] = v.v[k];
+                for (int k = 0; k < 8; k++) add[(team * 8 + k) * ROW + in_row] = v.v[k];
                 __syncthreads();
-                if (wave == 0) {
+                if (team == 0) {
 #pragma unroll
                     for (int k = 0; k < 8; k++)
-                        for (int o = 1; o < kJoinWaves; o++) v.v[k] += add[(o * 8 + k) * 64 + lane];
+                        for (int o = 1; o < TEAMS; o++) v.v[k] += add[(o * 8 + k) * ROW + in_row];
                 }
                 __syncthreads();
-                if (wave > 0) continue;
+                if (team > 0) continue;
             }
             if (c >= a.width) continue;           // (rows of sums are whole packs)
 #pragma unroll
@@ -370,31 +379,24 @@ struct DropoutArgs {
     void *y;
     const RowOf *row_of;
     int64_t ldx, ld_residual, ldy, columns;
-    uint32_t rows, units, blocks_a_row;           // packs of a row; workgroups of kBlock packs that a row has, where it has any
+    uint32_t items, units;                        // packs in all, and of a row
+    uint32_t factor, shift;                       // pack / units = pack * factor >> shift
     Dropout drop;
 };
 
-// A work item makes eight columns of a row.  Rows of fewer packs than a workgroup has lanes follow one another.
+// A work item makes eight columns of a row; the rows' packs follow one another without a gap (4160 columns are 520 packs, and
+// workgroups that begin with a row left a third of their lanes without any).
 template <class T>
 __global__ __launch_bounds__(kBlock) void k_dropout(const DropoutArgs a)
 {
     using E = typename T::elem;
-    uint32_t row, unit;
-    if (a.blocks_a_row) {
-        row = blockIdx.x / a.blocks_a_row;
-        unit = (blockIdx.x - row * a.blocks_a_row) * kBlock + threadIdx.x;
-    } else {
-        const uint32_t in = kBlock / a.units;     // rows of a workgroup
-        const uint32_t r = threadIdx.x / a.units;
-        if (r >= in) return;
-        row = blockIdx.x * in + r;
-        unit = threadIdx.x - r * a.units;
-    }
-    if (row >= a.rows || unit >= a.units) return;
+    const uint32_t p = blockIdx.x * kBlock + threadIdx.x;
+    if (p >= a.items) return;
+    const uint32_t row = (uint32_t)((uint64_t)p * a.factor >> a.shift), unit = p - row * a.units;
     const int64_t c = (int64_t)unit * 8, left = a.columns - c;
     const int valid = left < 8 ? (int)left : 8;
-    Eight v = load_eight<T>((const E *)a.x + row * a.ldx + c, valid), res = {};
-    if (a.residual) res = load_eight<T>((const E *)a.residual + row * a.ld_residual + c, valid);
+    Eight v = load_eight<T>((const E *)a.x + (int64_t)row * a.ldx + c, valid), res = {};
+    if (a.residual) res = load_eight<T>((const E *)a.residual + (int64_t)row * a.ld_residual + c, valid);
     const RowOf of = a.row_of[row];
     const Eight k = dropout_factors(a.drop, of.id, of.token, unit);
 #pragma unroll
@@ -402,29 +404,29 @@ __global__ __launch_bounds__(kBlock) void k_dropout(const DropoutArgs a)
         v.v[i] = kept(v.v[i], k.v[i]);
         if (a.residual) v.v[i] += res.v[i];
     }
-    store_eight<T>((E *)a.y + row * a.ldy + c, v, valid);
+    store_eight<T>((E *)a.y + (int64_t)row * a.ldy + c, v, valid);
 }
 
-// Wavefronts and packs of a lane that hold a row.  The forward kernel has a wavefront up to 2048 columns (no barriers, four loads of
-// a row in flight in each lane); the gradient's sums and rows would be more registers than a lane has.
-template <bool GRADIENT, class F>
+// Wavefronts and packs of a lane that hold a row.  With four packs a lane one wavefront has 2048 columns and meets no other, but the
+// registers leave half as many rows on their way: 14336 x 2048 bf16 forward 71 us, with two wavefronts of two packs 58 (4.1 TB/s).
+template <class F>
 void by_width(int64_t width, F launch)
 {
     const int64_t packs = (width + 7) / 8;
     if (packs <= 64) launch(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
     else if (packs <= 128) launch(std::integral_constant<int, 1>(), std::integral_constant<int, 2>());
-    else if (packs <= 256) launch(std::integral_constant<int, GRADIENT ? 2 : 1>(), std::integral_constant<int, GRADIENT ? 2 : 4>());
+    else if (packs <= 256) launch(std::integral_constant<int, 2>(), std::integral_constant<int, 2>());
     else if (packs <= 512) launch(std::integral_constant<int, 4>(), std::integral_constant<int, 2>());
     else if (packs <= 1024) launch(std::integral_constant<int, 8>(), std::integral_constant<int, 2>());
     else launch(std::integral_constant<int, 16>(), std::integral_constant<int, 2>());
 }
 
-inline int row_threads(int64_t width) { return width <= 2048 ? 64 : width <= 4096 ? 256 : width <= 8192 ? 512 : 1024; }
+inline int row_threads(int64_t width) { return width <= 1024 ? 64 : width <= 2048 ? 128 : width <= 4096 ? 256 : width <= 8192 ? 512 : 1024; }
 
 template <class T, bool CENTRED>
 int run_join(const JoinArgs &a, hipStream_t st)
 {
-    by_width<false>(a.width, [&](auto waves, auto packs) {
+    by_width(a.width, [&](auto waves, auto packs) {
         constexpr int W = decltype(waves)::value, P = decltype(packs)::value;
         k_join<T, CENTRED, W, P><<<W > 1 ? a.rows : cdiv(a.rows, kJoinWaves), 64 * (W > 1 ? W : kJoinWaves), 0, st>>>(a);
     });
@@ -435,9 +437,9 @@ template <class T, bool CENTRED>
 int run_gradient(const ccdc_block_t *b, const JoinArgs &a, const LearnedArgs &l, hipStream_t st)
 {
     if (!b->chunks.empty()) {
-        by_width<true>(a.width, [&](auto waves, auto packs) {
+        by_width(a.width, [&](auto waves, auto packs) {
             constexpr int W = decltype(waves)::value, P = decltype(packs)::value;
-            k_join_gradient<T, CENTRED, W, P><<<(uint32_t)b->chunks.size(), 64 * (W > 1 ? W : kJoinWaves), 0, st>>>(a);
+            k_join_gradient<T, CENTRED, W, P><<<(uint32_t)b->chunks.size(), 64 * W * teams(W), 0, st>>>(a);
         });
         const int rc = launched();
         if (rc != CCDC_OK) return rc;
@@ -455,9 +457,9 @@ int run_gradient(const ccdc_block_t *b, const JoinArgs &a, const LearnedArgs &l,
 }
 
 template <class T>
-int run_dropout(const DropoutArgs &a, uint32_t blocks, hipStream_t st)
+int run_dropout(const DropoutArgs &a, hipStream_t st)
 {
-    k_dropout<T><<<blocks, kBlock, 0, st>>>(a);
+    k_dropout<T><<<cdiv(a.items, kBlock), kBlock, 0, st>>>(a);
     return launched();
 }
 
@@ -499,7 +501,7 @@ int ccdc_join_backward(const ccdc_block_t *b, const void *dn, const void *dr, co
     for (const void *p : {dn, dr, y, f, w_post, gate, w_pre, (const void *)dx, (const void *)df, (const void *)dw_post,
                           (const void *)dgate, (const void *)dw_pre})
         if (!fits(b, p, true)) return CCDC_EINVAL;
-    if (b->c.width > kJoinWidth || !fits_launch((uint64_t)b->chunks.size() * std::max(row_threads(b->c.width), 64 * kJoinWaves)))
+    if (b->c.width > kJoinWidth || !fits_launch((uint64_t)b->chunks.size() * std::max(row_threads(b->c.width), 512)))
         return CCDC_ESIZE;
     JoinArgs a{};
     a.x = dr, a.dn = dn, a.y_in = y, a.f = f, a.w_post = w_post, a.gate = gate, a.w_pre = w_pre, a.y = dx, a.n = df;
@@ -524,15 +526,15 @@ int ccdc_dropout(const ccdc_block_t *b, int64_t rows, int64_t columns, double p,
     if (ldx < columns || ldy < columns || (residual && ld_residual < columns)) return CCDC_EINVAL;
     if (rows == 0) return CCDC_OK;
     if (!fits(b, x) || !fits(b, y) || !fits(b, residual, true)) return CCDC_EINVAL;
-    const int64_t units = (columns + 7) / 8;
-    if (units > INT32_MAX) return CCDC_ESIZE;
-    DropoutArgs a{x, residual, y, b->d_row_of, ldx, ld_residual, ldy, columns, (uint32_t)rows, (uint32_t)units, 0,
-                  make_dropout(p, site, seed)};
-    // a row's last workgroup may be short: rows share workgroups instead where they have less than a workgroup's packs
-    a.blocks_a_row = units <= kBlock ? 0 : cdiv(units, kBlock);
-    const uint64_t blocks = a.blocks_a_row ? (uint64_t)rows * a.blocks_a_row : cdiv(rows, kBlock / (uint32_t)units);
-    if (!fits_launch(blocks * kBlock)) return CCDC_ESIZE;
-    CCDC_BY_ELEM(b, (run_dropout<T>(a, (uint32_t)blocks, (hipStream_t)stream)));
+    const uint64_t units = ((uint64_t)columns + 7) / 8;
+    if (units > kMaxLaunchItems || !fits_launch(cdiv((uint64_t)rows * units, kBlock) * (uint64_t)kBlock)) return CCDC_ESIZE;
+    // exact for numbers below 2^31: with 2^bits >= units the factor is at most units - 1 too large times 2^-(31 + bits) of them
+    uint32_t bits = 0;
+    while (((uint64_t)1 << bits) < units) bits++;
+    const uint64_t factor = (((uint64_t)1 << (31 + bits)) + units - 1) / units;
+    const DropoutArgs a{x, residual, y, b->d_row_of, ldx, ld_residual, ldy, columns, (uint32_t)((uint64_t)rows * units), (uint32_t)units,
+                        (uint32_t)factor, 31 + bits, make_dropout(p, site, seed)};
+    CCDC_BY_ELEM(b, (run_dropout<T>(a, (hipStream_t)stream)));
 }
 
 }  // extern "C"

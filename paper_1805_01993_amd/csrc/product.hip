@@ -135,15 +135,15 @@ __device__ __forceinline__ Bits8 piece(CCDC_LDS unsigned char *lds, int row0, in
     }
 }
 
-// WN x WM wavefronts, each SN x SM pieces.
-template <class T, Product WHAT, int WN, int WM, int SN, int SM>
+// WN x WM wavefronts, each SN x SM pieces; BUFFERS steps in LDS.
+template <class T, Product WHAT, int WN, int WM, int SN, int SM, int BUFFERS>
 __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
 {
     constexpr bool NS = WHAT != Product::gated && WHAT != Product::plain, MS = WHAT == Product::weight_gradient;
     constexpr bool GATED = WHAT == Product::gated;
     constexpr int THREADS = 64 * WN * WM, TN = WN * SN * 32, TM = WM * SM * 32;
     constexpr int STEP = 64, BUFFER = (TN + TM) * STEP * 2;
-    __shared__ __attribute__((aligned(1024))) unsigned char memory[2 * BUFFER];
+    __shared__ __attribute__((aligned(1024))) unsigned char memory[BUFFERS * BUFFER];
     CCDC_LDS unsigned char *lds = (CCDC_LDS unsigned char *)memory;
     const uint32_t lds_at = (uint32_t)(uintptr_t)lds;
 
@@ -201,11 +201,11 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
             if (++at.segment == a.segments) at.segment = 0, at.planes++;
         }
     };
-    const auto copy_n = [&](int32_t s) { copies(cn, sn, next_n, true, s % 2 * BUFFER); };
-    const auto copy_m = [&](int32_t s) { copies(cm, sm, next_m, false, s % 2 * BUFFER); };
+    const auto copy_n = [&](int32_t s) { copies(cn, sn, next_n, true, s % BUFFERS * BUFFER); };
+    const auto copy_m = [&](int32_t s) { copies(cm, sm, next_m, false, s % BUFFERS * BUFFER); };
 
-    const auto piece_n = [&](int32_t s, int i, int k) { return piece<NS, TN, STEP>(lds + s % 2 * BUFFER, wn + i * 32, k); };
-    const auto piece_m = [&](int32_t s, int j, int k) { return piece<MS, TM, STEP>(lds + s % 2 * BUFFER + TN * STEP * 2, wm + j * 32, k); };
+    const auto piece_n = [&](int32_t s, int i, int k) { return piece<NS, TN, STEP>(lds + s % BUFFERS * BUFFER, wn + i * 32, k); };
+    const auto piece_m = [&](int32_t s, int j, int k) { return piece<MS, TM, STEP>(lds + s % BUFFERS * BUFFER + TN * STEP * 2, wm + j * 32, k); };
     const auto meet = [] {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_barrier" ::: "memory");
@@ -217,7 +217,8 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
         if (but_n) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(cn)::count) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     };
-    if constexpr (THREADS == 512) {
+    if constexpr (SM == 4) {
+        static_assert(THREADS == 512);
         // Two wavefronts a SIMD, the second of each a phase behind: while one reads pieces, the other multiplies its own, and
         // they change over at a barrier.  A wavefront has two turns a step: it reads all its pieces of side N and half
         // of side M, then the other half.  So N is free for the step after the next when the second of the two has had its first
@@ -264,9 +265,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
         }
         if (!second) meet();
     } else {
-        // One wavefront a SIMD, two workgroups a CU.  The pieces of the next 16 k are read while these are multiplied, the
-        // first of a step during the last of the step before: by then its copies are waited for, and with that barrier every
-        // wavefront has read all of the buffer, which the step after it is copied to.
+        // Two wavefronts a SIMD, and two workgroups a CU where there are as many.  The pieces of the next 16 k are read while these are
+        // multiplied, the first of a step during the last of the step before: by then its copies are waited for, and with that
+        // barrier every wavefront has read all of the buffer, which the next step to be copied goes to.
         Bits8 pn[2][SN], pm[2][SM];
         const auto read = [&](int to, int32_t s, int k) {
 #pragma unroll
@@ -278,11 +279,17 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
             copy_n(s);
             copy_m(s);
         };
+        static constexpr int kCopies = decltype(cn)::count + decltype(cm)::count;       // a wavefront's in each step
+        const auto there = [](int32_t later) {               // reads, and copies but those of the `later` last steps
+            if (BUFFERS > 2 && later >= 3) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(3 * kCopies) : "memory");
+            else if (BUFFERS > 2 && later == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * kCopies) : "memory");
+            else if (later == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kCopies) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        };
         if (steps > 0) {
-            copy(0);
-            all_there(false);
+            for (int32_t s = 0; s < min(steps, BUFFERS); s++) copy(s);
+            there(min(steps, BUFFERS) - 1);
             meet();
-            if (steps > 1) copy(1);
             read(0, 0, 0);
         }
         for (int32_t s = 0; s < steps; s++) {
@@ -291,9 +298,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
                 if (k + 1 < STEP / 16) {
                     read((k + 1) % 2, s, (k + 1) * 16);
                 } else if (s + 1 < steps) {
-                    all_there(false);
+                    there(min(steps - 2 - s, BUFFERS - 2));
                     meet();
-                    if (s + 2 < steps) copy(s);
+                    if (s + BUFFERS < steps) copy(s);
                     read(0, s + 1, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);       // left to itself the compiler puts the reads after the products
@@ -314,7 +321,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
     constexpr bool NARROW = sizeof(E) == 2 && WHAT != Product::gated && WHAT != Product::gated_gradient;      // staged as stored
 #pragma unroll
     for (int j = 0; j < SM; j++) {
-        CCDC_LDS unsigned char *stage = lds + (wave * 2 + j % 2) * 8192;
+        CCDC_LDS unsigned char *stage = lds + (SM > 1 ? wave * 2 + j % 2 : wave) * 8192;
 #pragma unroll
         for (int i = 0; i < SN; i++)
 #pragma unroll
@@ -413,24 +420,27 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
     }
 }
 
-template <class T, Product WHAT, int WN, int WM, int SN, int SM>
+template <class T, Product WHAT, int WN, int WM, int SN, int SM, int BUFFERS>
 int launch(ProductArgs a, hipStream_t st)
 {
     a.tiles_n = cdiv(a.rows_n, WN * SN * 32 / (WHAT == Product::gated ? 2 : 1));
     a.tiles_m = cdiv(a.rows_m, WM * SM * 32);
     const uint64_t tiles = (uint64_t)a.tiles_n * a.tiles_m * a.files * a.halves;
     if (!fits_launch(tiles * 64 * WN * WM)) return CCDC_ESIZE;
-    k_product<T, WHAT, WN, WM, SN, SM><<<(uint32_t)tiles, 64 * WN * WM, 0, st>>>(a);
+    k_product<T, WHAT, WN, WM, SN, SM, BUFFERS><<<(uint32_t)tiles, 64 * WN * WM, 0, st>>>(a);
     return launched();
 }
 
-// 256 x 256 tiles where they fill the chip.
+// 256 x 256 tiles where they fill the chip, else 128 x 128, with more of a tile on its way where a CU has only one.
 template <class T, Product WHAT>
 int by_tile(const ProductArgs &a, hipStream_t st)
 {
-    const uint64_t large = (uint64_t)cdiv(a.rows_n, WHAT == Product::gated ? 128 : 256) * cdiv(a.rows_m, 256) * a.files * a.halves;
-    if (large >= 256) return launch<T, WHAT, 4, 2, 2, 4>(a, st);
-    return launch<T, WHAT, 2, 2, 2, 2>(a, st);
+    const auto tiles = [&](uint32_t size) {
+        return (uint64_t)cdiv(a.rows_n, WHAT == Product::gated ? size / 2 : size) * cdiv(a.rows_m, size) * a.files * a.halves;
+    };
+    if (tiles(256) >= 256) return launch<T, WHAT, 4, 2, 2, 4, 2>(a, st);
+    if (tiles(128) > 256) return launch<T, WHAT, 2, 4, 2, 1, 2>(a, st);
+    return launch<T, WHAT, 2, 4, 2, 1, 4>(a, st);
 }
 
 template <class T>
