@@ -142,7 +142,8 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
     constexpr bool NS = WHAT != Product::gated && WHAT != Product::plain, MS = WHAT == Product::weight_gradient;
     constexpr bool GATED = WHAT == Product::gated;
     constexpr int THREADS = 64 * WN * WM, TN = WN * SN * 32, TM = WM * SM * 32;
-    constexpr int STEP = 64, BUFFER = (TN + TM) * STEP * 2;
+    // fp32: a step has all planes of 32 k, so that each is copied and read once for the products that it is in
+    constexpr int PLANES = T::planes, STEP = PLANES == 1 ? 64 : 32, PLANE = (TN + TM) * STEP * 2, BUFFER = PLANES * PLANE;
     __shared__ __attribute__((aligned(1024))) unsigned char memory[BUFFERS * BUFFER];
     CCDC_LDS unsigned char *lds = (CCDC_LDS unsigned char *)memory;
     const uint32_t lds_at = (uint32_t)(uintptr_t)lds;
@@ -181,31 +182,31 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0.0f;
 
     // steps: planes of either side, then ranges of k, then k
-    const int32_t in_k = (K + STEP - 1) / STEP, steps = in_k * a.segments * (T::planes == 1 ? 1 : 6);
+    const int32_t in_k = (K + STEP - 1) / STEP, steps = in_k * a.segments;
     // What is copied next of a side: its place in the side's order of steps.
     struct Next {
-        int32_t k = 0, segment = 0, planes = 0;
+        int32_t k = 0, segment = 0;
     };
     Next next_n, next_m;
-    const auto copies = [&](const auto &side, const Side &s, Next &at, bool of_n, uint32_t buffer) {
+    const auto copies = [&](const auto &side, const Side &s, Next &at, uint32_t buffer) {
         constexpr bool strided = std::decay_t<decltype(side)>::strided;
-        int64_t from = at.segment ? s.segment : 0;
-        if constexpr (T::planes == 3)             // (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
-            from += (((of_n ? 0x001102 : 0x010120) >> (4 * at.planes)) & 15) * s.plane;
-        const int64_t k0 = (int64_t)at.k * STEP;
-        from += strided ? k0 * s.ld : k0;
+        const int64_t k0 = (int64_t)at.k * STEP, from = (at.segment ? s.segment : 0) + (strided ? k0 * s.ld : k0);
 #pragma unroll
-        for (int i = 0; i < std::decay_t<decltype(side)>::count; i++) side.issue(i, from, K - (int32_t)k0, buffer);
-        if (++at.k == in_k) {
-            at.k = 0;
-            if (++at.segment == a.segments) at.segment = 0, at.planes++;
-        }
+        for (int plane = 0; plane < PLANES; plane++)
+#pragma unroll
+            for (int i = 0; i < std::decay_t<decltype(side)>::count; i++)
+                side.issue(i, from + plane * s.plane, K - (int32_t)k0, buffer + plane * PLANE);
+        if (++at.k == in_k) at.k = 0, at.segment++;
     };
-    const auto copy_n = [&](int32_t s) { copies(cn, sn, next_n, true, s % BUFFERS * BUFFER); };
-    const auto copy_m = [&](int32_t s) { copies(cm, sm, next_m, false, s % BUFFERS * BUFFER); };
+    const auto copy_n = [&](int32_t s) { copies(cn, sn, next_n, s % BUFFERS * BUFFER); };
+    const auto copy_m = [&](int32_t s) { copies(cm, sm, next_m, s % BUFFERS * BUFFER); };
 
-    const auto piece_n = [&](int32_t s, int i, int k) { return piece<NS, TN, STEP>(lds + s % BUFFERS * BUFFER, wn + i * 32, k); };
-    const auto piece_m = [&](int32_t s, int j, int k) { return piece<MS, TM, STEP>(lds + s % BUFFERS * BUFFER + TN * STEP * 2, wm + j * 32, k); };
+    const auto piece_n = [&](int32_t s, int i, int k, int plane = 0) {
+        return piece<NS, TN, STEP>(lds + s % BUFFERS * BUFFER + plane * PLANE, wn + i * 32, k);
+    };
+    const auto piece_m = [&](int32_t s, int j, int k, int plane = 0) {
+        return piece<MS, TM, STEP>(lds + s % BUFFERS * BUFFER + plane * PLANE + TN * STEP * 2, wm + j * 32, k);
+    };
     const auto meet = [] {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_barrier" ::: "memory");
@@ -268,18 +269,43 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
         // Two wavefronts a SIMD, and two workgroups a CU where there are as many.  The pieces of the next 16 k are read while these are
         // multiplied, the first of a step during the last of the step before: by then its copies are waited for, and with that
         // barrier every wavefront has read all of the buffer, which the next step to be copied goes to.
-        Bits8 pn[2][SN], pm[2][SM];
+        Bits8 pn[2][PLANES][SN], pm[2][PLANES][SM];
         const auto read = [&](int to, int32_t s, int k) {
 #pragma unroll
-            for (int i = 0; i < SN; i++) pn[to][i] = piece_n(s, i, k);
+            for (int p = 0; p < PLANES; p++) {
 #pragma unroll
-            for (int j = 0; j < SM; j++) pm[to][j] = piece_m(s, j, k);
+                for (int i = 0; i < SN; i++) pn[to][p][i] = piece_n(s, i, k, p);
+#pragma unroll
+                for (int j = 0; j < SM; j++) pm[to][p][j] = piece_m(s, j, k, p);
+            }
+        };
+        // fp32: the products of the parts but the first have sums of their own, in which they are not rounded to the first's last place
+        Acc small[PLANES == 3 ? SN : 1][PLANES == 3 ? SM : 1];
+        if constexpr (PLANES == 3)
+#pragma unroll
+            for (int i = 0; i < SN; i++)
+#pragma unroll
+                for (int j = 0; j < SM; j++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++) small[i][j][e] = 0.0f;
+        const auto products = [&](int of) {
+#pragma unroll
+            for (int q = PLANES == 3 ? 0 : 5; q < 6; q++) {       // parts (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
+                const int n = (0x001102 >> (4 * q)) & 15, m = (0x010120 >> (4 * q)) & 15;
+#pragma unroll
+                for (int i = 0; i < SN; i++)
+#pragma unroll
+                    for (int j = 0; j < SM; j++) {
+                        Acc &c = q < 5 ? small[PLANES == 3 ? i : 0][PLANES == 3 ? j : 0] : acc[i][j];
+                        c = multiply<T>(pn[of][n][i], pm[of][m][j], c);
+                    }
+            }
         };
         const auto copy = [&](int32_t s) {
             copy_n(s);
             copy_m(s);
         };
-        static constexpr int kCopies = decltype(cn)::count + decltype(cm)::count;       // a wavefront's in each step
+        static constexpr int kCopies = PLANES * (decltype(cn)::count + decltype(cm)::count);       // a wavefront's in each step
         const auto there = [](int32_t later) {               // reads, and copies but those of the `later` last steps
             if (BUFFERS > 2 && later >= 3) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(3 * kCopies) : "memory");
             else if (BUFFERS > 2 && later == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * kCopies) : "memory");
@@ -304,13 +330,15 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
                     read(0, s + 1, 0);
                 }
                 __builtin_amdgcn_sched_barrier(0);       // left to itself the compiler puts the reads after the products
-#pragma unroll
-                for (int i = 0; i < SN; i++)
-#pragma unroll
-                    for (int j = 0; j < SM; j++) acc[i][j] = multiply<T>(pn[k % 2][i], pm[k % 2][j], acc[i][j]);
+                products(k % 2);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+        if constexpr (PLANES == 3)
+#pragma unroll
+            for (int i = 0; i < SN; i++)
+#pragma unroll
+                for (int j = 0; j < SM; j++) acc[i][j] += small[i][j];
         meet();
     }
 
@@ -435,12 +463,16 @@ int launch(ProductArgs a, hipStream_t st)
 template <class T, Product WHAT>
 int by_tile(const ProductArgs &a, hipStream_t st)
 {
-    const auto tiles = [&](uint32_t size) {
-        return (uint64_t)cdiv(a.rows_n, WHAT == Product::gated ? size / 2 : size) * cdiv(a.rows_m, size) * a.files * a.halves;
-    };
-    if (tiles(256) >= 256) return launch<T, WHAT, 4, 2, 2, 4, 2>(a, st);
-    if (tiles(128) > 256) return launch<T, WHAT, 2, 4, 2, 1, 2>(a, st);
-    return launch<T, WHAT, 2, 4, 2, 1, 4>(a, st);
+    if constexpr (T::planes == 3) {
+        return launch<T, WHAT, 2, 4, 2, 1, 3>(a, st);
+    } else {
+        const auto tiles = [&](uint32_t size) {
+            return (uint64_t)cdiv(a.rows_n, WHAT == Product::gated ? size / 2 : size) * cdiv(a.rows_m, size) * a.files * a.halves;
+        };
+        if (tiles(256) >= 256) return launch<T, WHAT, 4, 2, 2, 4, 2>(a, st);
+        if (tiles(128) > 256) return launch<T, WHAT, 2, 4, 2, 1, 2>(a, st);
+        return launch<T, WHAT, 2, 4, 2, 1, 4>(a, st);
+    }
 }
 
 template <class T>
