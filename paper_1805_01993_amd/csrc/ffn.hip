@@ -10,15 +10,25 @@ struct SideArgs {
     const void *from;
     uint16_t *to;
     int64_t rows, columns, ld, to_ld, plane;
-    uint32_t packs;
+    uint32_t packs, blocks;               // of a row; workgroups up to the end of this matrix
+};
+constexpr int kMostSides = 4;
+struct SidesArgs {
+    SideArgs of[kMostSides];
+    int count;
 };
 
-// A matrix as a side of a product: fp32 numbers as their three parts, 16-bit ones that begin anywhere as rows of whole packs,
-// zeros past their ends.  A work item makes a pack.  Bound by memory (fp32: four bytes read and six written an element).
+// Matrices as sides of products: fp32 numbers as their three parts, 16-bit ones that begin anywhere as rows of whole packs,
+// zeros past their ends.  A work item makes a pack; all matrices of a call in one launch (56 files of 37 tokens, 515 x 1333 bf16, four
+// launches of 4 us each).  Bound by memory (fp32: four bytes read and six written an element).
 template <class T>
-__global__ __launch_bounds__(kBlock) void k_side(const SideArgs a)
+__global__ __launch_bounds__(kBlock) void k_sides(const SidesArgs all)
 {
-    const uint64_t p = (uint64_t)blockIdx.x * kBlock + threadIdx.x, row = p / a.packs;
+    int which = 0;
+    while (which + 1 < all.count && blockIdx.x >= all.of[which].blocks) which++;
+    const SideArgs &a = all.of[which];
+    const uint32_t first = which ? all.of[which - 1].blocks : 0;
+    const uint64_t p = (uint64_t)(blockIdx.x - first) * kBlock + threadIdx.x, row = p / a.packs;
     const uint32_t c = (uint32_t)(p - row * a.packs) * 8;
     if (row >= (uint64_t)a.rows) return;
     const Eight v = load_eight<T>((const typename T::elem *)a.from + row * a.ld + c, (int)min(a.columns - c, (int64_t)8));
@@ -26,33 +36,43 @@ __global__ __launch_bounds__(kBlock) void k_side(const SideArgs a)
 }
 
 template <class T>
-int run_side(const SideArgs &a, hipStream_t st)
+int run_sides(const SidesArgs &a, hipStream_t st)
 {
-    const uint64_t packs = (uint64_t)a.rows * a.packs;
-    if (!fits_launch(packs)) return CCDC_ESIZE;
-    k_side<T><<<cdiv(packs, kBlock), kBlock, 0, st>>>(a);
+    k_sides<T><<<a.of[a.count - 1].blocks, kBlock, 0, st>>>(a);
     return launched();
 }
 
-// A matrix of the caller's as a side of a product: as it is where rows of 16-bit numbers are whole packs of 16 bytes, else made
-// at `room` bytes into the workspace by a launch of its own.
-struct Prepared {
-    Side side;
-    int rc;
-};
+// The caller's matrices as sides of products: as they are where rows of 16-bit numbers are whole packs of 16 bytes, else made
+// in the workspace by one launch.
+class Sides {
+public:
+    Sides(const ccdc_block_t *b, hipStream_t st) : b_(b), st_(st) {}
+    Side add(const void *p, int64_t ld, int64_t rows, int64_t columns, size_t room)
+    {
+        if (b_->planes == 1 && columns % 8 == 0 && ld % 8 == 0 && aligned(p, 16)) return {(const uint16_t *)p, ld, 0, 0, (int32_t)columns};
+        const int64_t wide = padded(columns);
+        uint16_t *to = inside_of<uint16_t>(b_->d_workspace, room);
+        const uint32_t packs = (uint32_t)(wide / 8);
+        if (rows > 0) {
+            blocks_ += cdiv((uint64_t)rows * packs, kBlock);
+            sides_.of[sides_.count++] = {p, to, rows, columns, ld, wide, rows * wide, packs, (uint32_t)blocks_};
+        }
+        return {to, wide, rows * wide, 0, (int32_t)wide};
+    }
+    int make()
+    {
+        if (sides_.count == 0) return CCDC_OK;
+        if (!fits_launch(blocks_ * kBlock)) return CCDC_ESIZE;
+        const auto run = [&]() -> int { CCDC_BY_ELEM(b_, (run_sides<T>(sides_, st_))); };
+        return run();
+    }
 
-Prepared prepare(const ccdc_block_t *b, const void *p, int64_t ld, int64_t rows, int64_t columns, size_t room, hipStream_t st)
-{
-    Prepared out{{(const uint16_t *)p, ld, 0, 0, (int32_t)columns}, CCDC_OK};
-    if (b->planes == 1 && columns % 8 == 0 && ld % 8 == 0 && aligned(p, 16)) return out;
-    const int64_t wide = padded(columns);
-    uint16_t *to = inside_of<uint16_t>(b->d_workspace, room);
-    out.side = {to, wide, rows * wide, 0, (int32_t)wide};
-    const SideArgs a{p, to, rows, columns, ld, wide, rows * wide, (uint32_t)(wide / 8)};
-    const auto run = [&]() -> int { CCDC_BY_ELEM(b, (run_side<T>(a, st))); };
-    out.rc = rows > 0 ? run() : CCDC_OK;
-    return out;
-}
+private:
+    const ccdc_block_t *b_;
+    hipStream_t st_;
+    SidesArgs sides_{};
+    uint64_t blocks_ = 0;
+};
 
 // What every product of the block is given.
 ProductArgs common(const ccdc_block_t *b)
@@ -79,22 +99,23 @@ int forward(const ccdc_block_t *b, int64_t rows, const void *x, int64_t ldx, con
     const Dropout drop = make_dropout(b->c.dropout_hidden, 2 * b->c.layer, seed);
     if (!saved && rows <= kFewRows)
         return few_forward(b, rows, x, ldx, W_in, W_out, y, ldy, inside_of(b->d_workspace, b->at_h), drop, st);
-    const Prepared in = prepare(b, W_in, d, 2 * F, d, b->at_in, st), px = prepare(b, x, ldx, rows, d, b->at_x, st);
-    const Prepared out = prepare(b, W_out, F, d, F, b->at_out, st);
-    for (int rc : {in.rc, px.rc, out.rc})
-        if (rc != CCDC_OK) return rc;
+    Sides sides(b, st);
+    const Side in = sides.add(W_in, d, 2 * F, d, b->at_in), px = sides.add(x, ldx, rows, d, b->at_x);
+    const Side out = sides.add(W_out, F, d, F, b->at_out);
+    int rc = sides.make();
+    if (rc != CCDC_OK) return rc;
     uint16_t *h = saved ? inside_of<uint16_t>(saved, b->saved_h) : inside_of<uint16_t>(b->d_workspace, b->at_h);
     ProductArgs a = common(b);
-    a.n = in.side, a.m = px.side;
+    a.n = in, a.m = px;
     a.rows_n = (int32_t)F, a.rows_m = (int32_t)rows, a.K = (int32_t)padded(d);
     a.h = h;
     a.P = saved ? inside_of<float>(saved, b->saved_p) : nullptr;
     a.Q = saved ? inside_of<float>(saved, b->saved_q) : nullptr;
     a.drop = drop;
-    int rc = run_product(b->c.mode, Product::gated, a, st);
+    rc = run_product(b->c.mode, Product::gated, a, st);
     if (rc != CCDC_OK) return rc;
     a = common(b);
-    a.n = out.side, a.m = hidden_side(b, h);
+    a.n = out, a.m = hidden_side(b, h);
     a.rows_n = (int32_t)d, a.rows_m = (int32_t)rows, a.K = (int32_t)padded(F);
     a.c = y, a.ldc = ldy;
     return run_product(b->c.mode, Product::plain, a, st);
@@ -104,33 +125,35 @@ int backward(const ccdc_block_t *b, const void *x, int64_t ldx, const void *W_in
              int64_t lddy, void *dx, int64_t lddx, void *dW_in, int64_t ld_in, void *dW_out, int64_t ld_out, hipStream_t st)
 {
     const int64_t d = b->c.width, F = b->c.hidden, M = b->M, Fp = b->hidden_ld;
-    const Prepared out = prepare(b, W_out, F, d, F, b->at_out, st), pdy = prepare(b, dy, lddy, M, d, b->at_dy, st);
-    Prepared in{{}, CCDC_OK}, px{{}, CCDC_OK};
-    if (dx) in = prepare(b, W_in, d, 2 * F, d, b->at_in, st);
-    if (dW_in) px = prepare(b, x, ldx, M, d, b->at_x, st);
-    for (int rc : {out.rc, pdy.rc, in.rc, px.rc})
-        if (rc != CCDC_OK) return rc;
+    Sides sides(b, st);
+    const Side out = sides.add(W_out, F, d, F, b->at_out), pdy = sides.add(dy, lddy, M, d, b->at_dy);
+    Side in{}, px{};
+    if (dx) in = sides.add(W_in, d, 2 * F, d, b->at_in);
+    if (dW_in) px = sides.add(x, ldx, M, d, b->at_x);
+    int rc = sides.make();
+    if (rc != CCDC_OK) return rc;
     // gradients of a and u, side by side: as one range of 2 F where F is whole packs, else as two of F
     const bool one = F == Fp;
     uint16_t *dau = inside_of<uint16_t>(b->d_workspace, b->at_dau);
     ProductArgs a = common(b);
-    a.n = out.side, a.m = pdy.side;
+    a.n = out, a.m = pdy;
     a.rows_n = (int32_t)F, a.rows_m = (int32_t)M, a.K = (int32_t)d;
     a.h = dau, a.plane_h = M * 2 * Fp, a.second_h = Fp;
     a.P = inside_of<float>(saved, b->saved_p), a.Q = inside_of<float>(saved, b->saved_q);
-    int rc = run_product(b->c.mode, Product::gated_gradient, a, st);
+    rc = run_product(b->c.mode, Product::gated_gradient, a, st);
     if (rc != CCDC_OK) return rc;
     const Side both{dau, 2 * Fp, M * 2 * Fp, Fp, (int32_t)(one ? 2 * Fp : Fp)};
     if (dW_in) {
         // side N: x or h, side M: gradients, both with the tokens of a file as k
         a = common(b);
         a.first = b->d_first, a.files = b->N, a.file_c = ld_in;
-        a.n = px.side, a.m = both;
+        a.K = (int32_t)(M / b->N);
+        a.n = px, a.m = both;
         a.halves = one ? 1 : 2, a.half_c = F * d;
         a.rows_n = (int32_t)d, a.rows_m = (int32_t)(one ? 2 * F : F);
         a.c = dW_in, a.ldc = d;
         if ((rc = run_product(b->c.mode, Product::weight_gradient, a, st)) != CCDC_OK) return rc;
-        a.n = hidden_side(b, inside_of<uint16_t>(saved, b->saved_h)), a.m = pdy.side;
+        a.n = hidden_side(b, inside_of<uint16_t>(saved, b->saved_h)), a.m = pdy;
         a.halves = 1;
         a.rows_n = (int32_t)F, a.rows_m = (int32_t)d;
         a.c = dW_out, a.ldc = F, a.file_c = ld_out;
@@ -138,8 +161,8 @@ int backward(const ccdc_block_t *b, const void *x, int64_t ldx, const void *W_in
     }
     if (!dx) return CCDC_OK;
     a = common(b);
-    a.n = in.side, a.m = both;
-    a.n.segment = F * in.side.ld;
+    a.n = in, a.m = both;
+    a.n.segment = F * in.ld;
     a.segments = one ? 1 : 2;
     a.rows_n = (int32_t)d, a.rows_m = (int32_t)M, a.K = (int32_t)(one ? 2 * F : F);
     a.c = dx, a.ldc = lddx;

@@ -143,7 +143,8 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
     constexpr bool GATED = WHAT == Product::gated;
     constexpr int THREADS = 64 * WN * WM, TN = WN * SN * 32, TM = WM * SM * 32;
     // fp32: a step has all planes of 32 k, so that each is copied and read once for the products that it is in
-    constexpr int PLANES = T::planes, STEP = PLANES == 1 ? 64 : 32, PLANE = (TN + TM) * STEP * 2, BUFFER = PLANES * PLANE;
+    // (small tiles of gradients of weights: files are often shorter than 64 tokens, and with half the LDS a CU has three of them)
+    constexpr int PLANES = T::planes, STEP = PLANES == 3 || (WHAT == Product::weight_gradient && SM == 1) ? 32 : 64, PLANE = (TN + TM) * STEP * 2, BUFFER = PLANES * PLANE;
     __shared__ __attribute__((aligned(1024))) unsigned char memory[BUFFERS * BUFFER];
     CCDC_LDS unsigned char *lds = (CCDC_LDS unsigned char *)memory;
     const uint32_t lds_at = (uint32_t)(uintptr_t)lds;
@@ -349,7 +350,8 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
     constexpr bool NARROW = sizeof(E) == 2 && WHAT != Product::gated && WHAT != Product::gated_gradient;      // staged as stored
 #pragma unroll
     for (int j = 0; j < SM; j++) {
-        CCDC_LDS unsigned char *stage = lds + (SM > 1 ? wave * 2 + j % 2 : wave) * 8192;
+        CCDC_LDS unsigned char *stage = lds + (SM > 1 ? wave * 2 + j % 2 : wave) * (NARROW ? 4096 : 8192);
+        static_assert(BUFFERS * BUFFER >= WN * WM * (SM > 1 ? 2 : 1) * (NARROW ? 4096 : 8192));
 #pragma unroll
         for (int i = 0; i < SN; i++)
 #pragma unroll
@@ -459,19 +461,32 @@ int launch(ProductArgs a, hipStream_t st)
     return launched();
 }
 
-// 256 x 256 tiles where they fill the chip, else 128 x 128, with more of a tile on its way where a CU has only one.
+// Tiles of 256 x 256, one a CU, or of 128 x 128, two (16-bit numbers), by the rounds of them that the chip's 256 CUs make.  A round of large
+// ones is twice the work of a round of small ones in 1.75 of the time (2048 x 4160 bf16, a and u: 462 large tiles 178 us, 910 small ones
+// 102).  A tile of a gradient of weights is short, as its file is, and what comes before and after the products counts: with
+// 28 files of 64 tokens the small tiles took 0.90 of the time, of 128 1.03, of 512 1.25; 515 x 1333, where the large ones are a
+// quarter past the edge, 64 tokens 0.69, 256 0.86.
+template <Product WHAT>
+bool large_tiles(const ProductArgs &a)
+{
+    const auto rounds = [&](uint32_t size, uint32_t at_once) {
+        return (double)cdiv((uint64_t)cdiv(a.rows_n, WHAT == Product::gated ? size / 2 : size) * cdiv(a.rows_m, size) * a.files * a.halves, at_once);
+    };
+    double time = 1.75;
+    if (WHAT == Product::weight_gradient) time = a.K < 128 ? 2.2 : a.K < 256 ? 1.9 : 1.6;
+    return rounds(256, 256) * time <= rounds(128, 512);
+}
+
 template <class T, Product WHAT>
 int by_tile(const ProductArgs &a, hipStream_t st)
 {
     if constexpr (T::planes == 3) {
         return launch<T, WHAT, 2, 4, 2, 1, 3>(a, st);
     } else {
-        const auto tiles = [&](uint32_t size) {
-            return (uint64_t)cdiv(a.rows_n, WHAT == Product::gated ? size / 2 : size) * cdiv(a.rows_m, size) * a.files * a.halves;
-        };
-        if (tiles(256) >= 256) return launch<T, WHAT, 4, 2, 2, 4, 2>(a, st);
-        if (tiles(128) > 256) return launch<T, WHAT, 2, 4, 2, 1, 2>(a, st);
-        return launch<T, WHAT, 2, 4, 2, 1, 4>(a, st);
+        if (large_tiles<WHAT>(a)) return launch<T, WHAT, 4, 2, 2, 4, 2>(a, st);
+        const uint64_t small = (uint64_t)cdiv(a.rows_n, WHAT == Product::gated ? 64 : 128) * cdiv(a.rows_m, 128) * a.files * a.halves;
+        if (small > 256) return launch<T, WHAT, 2, 4, 2, 1, 2>(a, st);
+        return launch<T, WHAT, 2, 4, 2, 1, 4>(a, st);         // one a CU: with its LDS, more of a tile on its way
     }
 }
 

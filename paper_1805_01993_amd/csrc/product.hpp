@@ -26,7 +26,7 @@ enum class Product {
 struct ProductArgs {
     Side n, m;
     int32_t rows_n, rows_m;       // of the result; gated: rows_n is the hidden size
-    int32_t K, segments;
+    int32_t K, segments;          // weight_gradient: the files' tokens on average, for the choice of a tile
     int32_t tiles_n, tiles_m;
     const int32_t *first;         // weight_gradient: rows of k where the files begin
     int32_t files, halves;        // halves: products a file has, side M of the second from its segment on
