@@ -57,6 +57,8 @@ _CALLS = [("ccdc_pipeline_fused", False, "V X Phi"), ("ccdc_pipeline_fused_noall
           ("ccdc_map", False, "V Phi V"), ("ccdc_combine", False, "V Vbar"), ("ccdc_encode", False, "Vbar X"),
           ("ccdc_decode", False, "X Vbar D"), ("ccdc_reduce", False, "V D Phi"), ("ccdc_shuffle_fused", False, "V X D"),
           ("ccdc_node_encode", True, "V X"), ("ccdc_node_decode_reduce", True, "V X Phi")]
+_BLOCK_CALLS = ("ccdc_ffn_forward", "ccdc_ffn_backward", "ccdc_join_forward", "ccdc_join_backward", "ccdc_dropout")
+_FFN_FORWARD, _FFN_BACKWARD, _JOIN_FORWARD, _JOIN_BACKWARD, _DROPOUT = range(len(_BLOCK_CALLS))
 (_PIPELINE, _PIPELINE_NOALLOC, _MAP, _COMBINE, _ENCODE, _DECODE, _REDUCE, _SHUFFLE, _NODE_ENCODE,
  _NODE_DECODE) = range(len(_CALLS))
 
@@ -198,6 +200,10 @@ def _not_here(*args):
 
 def _failed(status, call):
     _check(status, _CALLS[call][0])
+
+
+def _block_failed(status, call):
+    _check(status, _BLOCK_CALLS[call])
 
 
 class Plan:
@@ -444,6 +450,7 @@ class Block:
     def __init__(self, width, hidden, mode, activation="silu", norm="rms", eps=1e-6, residual_scale=1.0,
                  dropout_hidden=0.0, dropout_out=0.0, layer=0):
         self._h = None
+        self._quick = _not_here
         lib = load_library()
         mode = MODES.get(mode, mode)
         config = BlockConfig(int(width), int(hidden), mode, ACTIVATIONS.get(activation, activation), NORMS.get(norm, norm),
@@ -457,6 +464,7 @@ class Block:
         self.tokens = self.files = self.saved_bytes = None
 
     def close(self):
+        self._quick = _not_here
         if getattr(self, "_h", None):
             self._lib.ccdc_block_destroy(self._h)
             self._h = None
@@ -476,6 +484,11 @@ class Block:
         _check(self._lib.ccdc_block_bind(self._h, len(tokens), (C.c_int64 * len(tokens))(*tokens), numbers), "ccdc_block_bind")
         self.tokens, self.files = self.query(BLOCK_Q_TOKENS), self.query(BLOCK_Q_FILES)
         self.saved_bytes = self.query(BLOCK_Q_SAVED_BYTES)
+        if _marshal is not None:
+            import torch
+            self._quick = _marshal.Block(
+                self._h.value, _block_failed, {torch.float32: 4, torch.float16: 3}.get(self.dtype, 2), self.width, self.hidden,
+                self.tokens, self.files, self.saved_bytes, *(C.cast(getattr(self._lib, f), C.c_void_p).value for f in _BLOCK_CALLS))
         return self
 
     def upload(self):
@@ -541,6 +554,8 @@ class Block:
     # ---- the block
     def ffn_forward(self, x, W_in, W_out, y, saved=None, seed=0, stream=None):
         """y = D(act(x Wg') x Wu') Wd'.  saved: a uint8 tensor of saved_bytes for ffn_backward."""
+        if stream is None and self._quick(_FFN_FORWARD, x, W_in, W_out, y, saved, seed) == OK:
+            return
         rows = x.shape[0]
         if saved is not None and (not saved.is_cuda or not saved.is_contiguous() or saved.numel() * saved.element_size() < self.saved_bytes):
             raise ValueError(f"saved: need {self.saved_bytes} contiguous bytes on the device")
@@ -553,6 +568,8 @@ class Block:
     def ffn_backward(self, x, W_in, W_out, saved, dy, dx, dW_in, dW_out, stream=None):
         """dx and, file by file, dW_in [files][2 hidden][width] and dW_out [files][width][hidden]; dx or both dW None: not
         wanted."""
+        if stream is None and self._quick(_FFN_BACKWARD, x, W_in, W_out, saved, dy, dx, dW_in, dW_out) == OK:
+            return
         if not saved.is_cuda or not saved.is_contiguous() or saved.numel() * saved.element_size() < self.saved_bytes:
             raise ValueError(f"saved: need {self.saved_bytes} contiguous bytes on the device")
         (din,), ld_in = self._gradients((("dW_in", dW_in, (2 * self.hidden, self.width)),))
@@ -572,6 +589,8 @@ class Block:
     def join_forward(self, x, f, y, n, w_post=None, gate=None, w_pre=None, seed=0, stream=None):
         """y = residual_scale x + gate D(norm(f; w_post)), n = norm(y; w_pre).  f, y, n None: without it; gate [width], or
         [files][width]."""
+        if stream is None and self._quick(_JOIN_FORWARD, x, f, y, n, w_post, gate, w_pre, seed) == OK:
+            return
         d, rows = self.width, x.shape[0]
         g, ld_gate = self._gate(gate)
         _check(self._lib.ccdc_join_forward(
@@ -582,6 +601,8 @@ class Block:
     def join_backward(self, dn, dr, y, f, dx, df, w_post=None, gate=None, w_pre=None, dw_post=None, dgate=None, dw_pre=None,
                       seed=0, stream=None):
         """From dn, the gradient of n, and dr, that of y by other ways: dx, df and per-file gradients [files][width]."""
+        if stream is None and self._quick(_JOIN_BACKWARD, dn, dr, y, f, dx, df, w_post, gate, w_pre, dw_post, dgate, dw_pre, seed) == OK:
+            return
         d, M = self.width, self.tokens
         g, ld_gate = self._gate(gate)
         grads, ld = self._gradients((("dw_post", dw_post, (d,)), ("dgate", dgate, (d,)), ("dw_pre", dw_pre, (d,))))
@@ -593,6 +614,8 @@ class Block:
 
     def dropout(self, x, y, p, site, seed=0, residual=None, stream=None):
         """y = D(x) + residual; the gradient of x is the same call on that of y."""
+        if stream is None and self._quick(_DROPOUT, x, y, p, site, seed, residual) == OK:
+            return
         rows, columns = x.shape
         _check(self._lib.ccdc_dropout(
             self._h, rows, columns, p, site, seed, self._matrix(x, "x", columns), self._ld(x),

@@ -408,6 +408,40 @@ def test_calls_on_two_streams(torch, L):
     assert all(torch.equal(a, b) for a, b in zip(alone, ys))
 
 
+@pytest.mark.parametrize("mode", MODES)
+def test_native_and_python_marshalling_agree(torch, L, mode):
+    """A call on torch's current stream is handed over natively, one that names a stream through ctypes: the same arguments."""
+    rng = np.random.default_rng(6)
+    d, F, lengths = 72, 88, [5, 0, 20]
+    block = L.ccdc_block(d, F, mode, dropout_hidden=0.1, dropout_out=0.2, residual_scale=0.5).bind(lengths).upload()
+    x, dy = (numbers(torch, mode, rng, (25, d), ld=d + 8)[0] for _ in range(2))
+    W_in, W_out = numbers(torch, mode, rng, (2 * F, d), 0.1)[0], numbers(torch, mode, rng, (d, F), 0.1)[0]
+    w, gate = numbers(torch, mode, rng, (d,))[0], numbers(torch, mode, rng, (3, d))[0]
+    saved = torch.empty(block.saved_bytes, dtype=torch.uint8, device="cuda")
+    quick, taken = block._quick, []
+
+    def watched(*args):
+        taken.append(quick(*args))
+        return taken[-1]
+
+    block._quick = watched
+    results = []
+    for stream in (None, torch.cuda.current_stream()):
+        y, z, n, dx, df, k = (empty(torch, x, 25, d, ld=d + 8) for _ in range(6))
+        rows, sums = empty(torch, x, 3, 3 * F * d + 4), empty(torch, x, 3, 3 * d)
+        dW_in, dW_out = rows[:, :2 * F * d].unflatten(1, (2 * F, d)), rows[:, 2 * F * d:3 * F * d].unflatten(1, (d, F))
+        block.ffn_forward(x, W_in, W_out, y, saved=saved, seed=SEED, stream=stream)
+        block.join_forward(x, y, z, n, w_post=w, gate=gate, w_pre=w, seed=SEED, stream=stream)
+        block.join_backward(dy, None, z, y, dx, df, w_post=w, gate=gate, w_pre=w, dw_post=sums[:, :d], dgate=sums[:, d:2 * d],
+                            dw_pre=sums[:, 2 * d:], seed=SEED, stream=stream)
+        block.ffn_backward(x, W_in, W_out, saved, df, dx, dW_in, dW_out, stream=stream)
+        block.dropout(x, k, 0.25, site=9, seed=SEED, residual=dy, stream=stream)
+        torch.cuda.synchronize()
+        results.append([t.clone() for t in (y, z, n, dx, df, k, rows[:, :3 * F * d], sums)])
+    assert taken == [0] * 5
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
 def test_a_training_step_in_a_graph(torch, L):
     rng = np.random.default_rng(4)
     d, F, lengths, mode = 136, 256, [50, 0, 33], "bf16"
