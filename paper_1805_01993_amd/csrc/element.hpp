@@ -42,29 +42,51 @@ __device__ __forceinline__ V fresh_uniform(V v)
 // 1 for the first `valid` of a pack's elements, else 0, without a mask.
 __device__ __forceinline__ int inside(int valid, int i) { return min(max(valid - i, 0), 1); }
 
-template <class T, bool KEPT = true>
-__device__ __forceinline__ Eight load_eight(const typename T::elem *p, int valid)
+// As loaded; zeros past the row's end.
+template <class T>
+struct Raw8 {
+    Pack<typename T::elem, 8> p;
+};
+
+template <class T>
+__device__ __forceinline__ Raw8<T> load_raw(const typename T::elem *p, int valid)
 {
     using E = typename T::elem;
     constexpr int W = 16 / sizeof(E);
     using P = Pack<E, W>;
-    Eight out;
+    Raw8<T> out;
     valid = fresh(valid);
     if (valid >= 8) {
 #pragma unroll
         for (int h = 0; h < 8 / W; h++) {
-            const P q = load_pack_any<KEPT, P, E>(p + h * W);
+            const P q = load_pack_any<true, P, E>(p + h * W);
 #pragma unroll
-            for (int i = 0; i < W; i++) out.v[h * W + i] = T::widen(q.v[i]);
+            for (int i = 0; i < W; i++) out.p.v[h * W + i] = q.v[i];
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const float v = T::widen(p[min(i, valid - 1)]);
-            out.v[i] = __int_as_float(__float_as_int(v) & -inside(valid, i));
+            const E e = p[min(i, valid - 1)];
+            if constexpr (sizeof(E) == 2) out.p.v[i] = (E)(e & -inside(valid, i));
+            else out.p.v[i] = __int_as_float(__float_as_int(e) & -inside(valid, i));
         }
     }
     return out;
+}
+
+template <class T>
+__device__ __forceinline__ Eight widen(const Raw8<T> &raw)
+{
+    Eight out;
+#pragma unroll
+    for (int i = 0; i < 8; i++) out.v[i] = T::widen(raw.p.v[i]);
+    return out;
+}
+
+template <class T>
+__device__ __forceinline__ Eight load_eight(const typename T::elem *p, int valid)
+{
+    return widen(load_raw<T>(p, valid));
 }
 
 template <class T, bool STREAM = false>
