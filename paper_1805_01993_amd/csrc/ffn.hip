@@ -192,12 +192,13 @@ int ccdc_ffn_backward(const ccdc_block_t *b, const void *x, int64_t ldx, const v
     const int rc = ready(b);
     if (rc != CCDC_OK) return rc;
     const int64_t d = b->c.width, F = b->c.hidden;
-    if ((!dx && !dW_in) || !dW_in != !dW_out || ldx < d || lddy < d || (dx && lddx < d)) return CCDC_EINVAL;
+    if ((!dx && !dW_in && b->M > 0) || !dW_in != !dW_out || ldx < d || lddy < d || (dx && lddx < d)) return CCDC_EINVAL;
     if (dW_in && b->N > 1 && (ld_in < 2 * F * d || ld_out < d * F)) return CCDC_EINVAL;
-    if (!fits(b, x) || !fits(b, W_in) || !fits(b, W_out) || !saved || !aligned(saved, 16) || !fits(b, dy) || !fits(b, dx, true) ||
-        !fits(b, dW_in, true) || !fits(b, dW_out, true))
+    const bool empty = b->M == 0;                 // a batch without tokens has no rows to point at; its gradients are zeros
+    if (!fits(b, x, empty) || !fits(b, W_in) || !fits(b, W_out) || !aligned(saved, 16) || (!saved && !empty) || !fits(b, dy, empty) ||
+        !fits(b, dx, true) || !fits(b, dW_in, true) || !fits(b, dW_out, true))
         return CCDC_EINVAL;
-    if (dx == dy && lddx != lddy) return CCDC_EINVAL;
+    if (dx && dx == dy && lddx != lddy) return CCDC_EINVAL;
     WorkspaceOrder order(b, (hipStream_t)stream, true);
     return backward(b, x, ldx, W_in, W_out, saved, dy, lddy, dx, lddx, dW_in, ld_in, dW_out, ld_out,
                     (hipStream_t)stream);

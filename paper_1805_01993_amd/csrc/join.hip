@@ -537,7 +537,8 @@ int ccdc_join_backward(const ccdc_block_t *b, const void *dn, const void *dr, co
     const int rc = ready(b);
     if (rc != CCDC_OK) return rc;
     const bool learned = dw_post || dgate || dw_pre;
-    if ((!dn && !dr) || (dn && !y) || (!f && (df || dw_post || dgate)) || (!dn && dw_pre)) return CCDC_EINVAL;
+    // (a batch without tokens has no rows to point at; its gradients are zeros)
+    if (b->M > 0 && ((!dn && !dr) || (dn && !y) || (!f && (df || dw_post || dgate)) || (!dn && dw_pre))) return CCDC_EINVAL;
     if (ld < b->c.width || (ld_gate != 0 && ld_gate < b->c.width) || (learned && b->N > 1 && ld_file < b->c.width)) return CCDC_EINVAL;
     for (const void *p : {dn, dr, y, f, w_post, gate, w_pre, (const void *)dx, (const void *)df, (const void *)dw_post,
                           (const void *)dgate, (const void *)dw_pre})

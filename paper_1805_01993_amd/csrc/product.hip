@@ -324,7 +324,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
             for (int k = 0; k < STEP / 16; k++) {
                 if (k + 1 < STEP / 16) {
                     read((k + 1) % 2, s, (k + 1) * 16);
-                } else if (s + 1 < steps) {
+                } else {
+                    // also after the last step, and what is read then is not used: behind a branch around the reads the compiler
+                    // would wait for all that are on their way
                     there(min(steps - 2 - s, BUFFERS - 2));
                     meet();
                     if (s + BUFFERS < steps) copy(s);
@@ -340,7 +342,6 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
             for (int i = 0; i < SN; i++)
 #pragma unroll
                 for (int j = 0; j < SM; j++) acc[i][j] += small[i][j];
-        meet();
     }
 
     // The result goes through LDS, a wavefront's rows of 64 n at a time, each by itself: an accumulator's lanes have four n of 32 rows,

@@ -196,6 +196,24 @@ def test_a_files_gradients_are_the_same_in_every_batch(torch, L, mode):
                 assert torch.equal(a, b), f"file {n} in {files}: gradient {i} differs"
 
 
+@pytest.mark.parametrize("mode", MODES)
+def test_a_batch_without_tokens(torch, L, mode):
+    """Files, but no token in any: nothing to compute, and gradients of zeros."""
+    d, F = 24, 40
+    block = L.ccdc_block(d, F, mode).bind([0, 0, 0]).upload()
+    new = lambda *s: torch.full(s, float("nan"), dtype=block.dtype, device="cuda")  # noqa: E731
+    none, W_in, W_out, w = new(0, d), new(2 * F, d).zero_(), new(d, F).zero_(), new(d).zero_()
+    saved = torch.empty(block.saved_bytes, dtype=torch.uint8, device="cuda")
+    dW_in, dW_out, sums = new(3, 2 * F, d), new(3, d, F), [new(3, d) for _ in range(3)]
+    block.ffn_forward(none, W_in, W_out, none, saved=saved)
+    block.ffn_backward(none, W_in, W_out, saved, none, none, dW_in, dW_out)
+    block.join_forward(none, none, none, none, w_post=w, gate=w, w_pre=w)
+    block.join_backward(none, none, none, none, none, none, w_post=w, gate=w, w_pre=w, dw_post=sums[0], dgate=sums[1], dw_pre=sums[2])
+    block.dropout(none, none, 0.5, site=0)
+    torch.cuda.synchronize()
+    assert all((t == 0).all() for t in [dW_in, dW_out] + sums)
+
+
 # ------------------------------------------------------------------ joins
 def run_join(torch, L, lengths, d, mode, centred=False, p=0.0, gate="shared", parts="xfn", ld=None, parameters=True):
     rng = np.random.default_rng(d + len(lengths))
