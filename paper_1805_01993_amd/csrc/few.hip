@@ -103,8 +103,7 @@ template <class T, bool GATED, int S, int MT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_few(const FewArgs a)
 {
     using E = typename T::elem;
-    constexpr int R = 16 / S, STREAMS = GATED ? 2 : 1, STEP = 32 * S, COLUMNS = MT * 16 / S, AHEAD = T::planes == 3 ? (MT > 2 ? 1 : 2) : MT > 1 ? 2 : 4;
-    static_assert(S == 1 || MT == 1);
+    constexpr int R = 16 / S, STREAMS = GATED ? 2 : 1, STEP = 32 * S, COLUMNS = MT * 16 / S, AHEAD = T::planes == 3 ? (MT > 2 ? 1 : 2) : MT > 4 ? 1 : MT > 1 ? 2 : 4;
     __shared__ float sums[WAVES][STREAMS][MT][16][17];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16;
     const int32_t n0 = blockIdx.x * R, offset = r % S * 32 + lane / 16 * 8;
@@ -113,7 +112,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_few(const FewArgs a)
     for (int i = 0; i < STREAMS; i++)
         w[i] = (const E *)a.w + ((int64_t)min(n0 + r / S, a.rows_n - 1) + (i ? a.rows_n : 0)) * a.ldw + offset;
 #pragma unroll
-    for (int t = 0; t < MT; t++) x[t] = (const E *)a.x + (int64_t)min(t * 16 + r / S, a.rows_m - 1) * a.ldx + offset;
+    for (int t = 0; t < MT; t++) x[t] = (const E *)a.x + (int64_t)min(t * R + r / S, a.rows_m - 1) * a.ldx + offset;
 
     Acc4 acc[STREAMS][MT] = {};
     const int32_t whole = a.K / STEP;
@@ -203,11 +202,14 @@ int run_few(const FewArgs &a, hipStream_t st)
         return launched();
     };
     using std::integral_constant;
+    constexpr bool wide = T::planes == 3;         // three times the registers an operand: no parts for more than sixteen rows
     if (a.rows_m <= 4) return go(integral_constant<int, 4>(), integral_constant<int, 1>(), integral_constant<int, GATED ? 4 : 8>());
     if (a.rows_m <= 8) return go(integral_constant<int, 2>(), integral_constant<int, 1>(), integral_constant<int, 8>());
-    if (a.rows_m <= 16) return go(integral_constant<int, 1>(), integral_constant<int, 1>(), integral_constant<int, GATED ? 8 : 16>());
-    if (a.rows_m <= 32) return go(integral_constant<int, 1>(), integral_constant<int, 2>(), integral_constant<int, GATED ? 8 : 16>());
-    return go(integral_constant<int, 1>(), integral_constant<int, 4>(), integral_constant<int, 8>());
+    if (a.rows_m <= 16) return go(integral_constant<int, 2>(), integral_constant<int, 2>(), integral_constant<int, GATED ? 8 : 16>());
+    if (a.rows_m <= 32)
+        return go(integral_constant<int, wide ? 1 : 2>(), integral_constant<int, wide ? 2 : 4>(),
+                  integral_constant<int, !GATED ? 16 : wide ? 8 : 4>());
+    return go(integral_constant<int, wide ? 1 : 2>(), integral_constant<int, wide ? 4 : 8>(), integral_constant<int, GATED && !wide ? 4 : 8>());
 }
 
 }  // namespace
