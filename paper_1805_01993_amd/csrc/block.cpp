@@ -73,6 +73,7 @@ int bind_block(ccdc_block_t *b, int files, const int64_t *tokens, const int32_t 
     b->at_dy = take(&at, M * width_ld * operand);
     b->at_in = take(&at, 2 * b->c.hidden * width_ld * operand);
     b->at_out = take(&at, b->c.width * hidden_ld * operand);
+    b->at_parts = take(&at, (M * width_ld < kPartElements / 256 ? M * width_ld * 256 : kPartElements) * 4);
     size_t sums = 0;
     if (b->c.width <= kJoinWidth) take(&sums, (int64_t)chunks.size() * 2 * width_ld * 4);
     b->workspace_bytes = at > sums ? at : sums;

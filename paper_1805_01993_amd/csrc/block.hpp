@@ -24,6 +24,9 @@ struct Chunk {
 constexpr int kChunkRows = 32;
 constexpr int64_t kJoinWidth = 16384;         // widest rows that one workgroup holds in registers
 
+// Elements of y in all ranges of k together where its product is cut into some: those of 256 tiles.
+constexpr int64_t kPartElements = (int64_t)256 * 128 * 128;
+
 constexpr int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
 
 }  // namespace ccdc
@@ -45,7 +48,7 @@ struct ccdc_block_s {
 
     // bytes from the workspace's beginning: hidden values; gradients of a and u; x, dy, W_in and W_out where products do
     // not take them as they are; sums of the chunks (over all of these)
-    size_t at_h = 0, at_dau = 0, at_x = 0, at_dy = 0, at_in = 0, at_out = 0, workspace_bytes = 0;
+    size_t at_h = 0, at_dau = 0, at_x = 0, at_dy = 0, at_in = 0, at_out = 0, at_parts = 0, workspace_bytes = 0;
     size_t saved_h = 0, saved_p = 0, saved_q = 0, saved_bytes = 0;
 
     bool uploaded = false;

@@ -74,6 +74,45 @@ private:
     uint64_t blocks_ = 0;
 };
 
+struct PartsArgs {
+    const float *parts;
+    void *y;
+    int64_t part, ld, ldy;
+    int32_t count, width;
+    uint32_t rows, packs;
+};
+
+// y from its ranges of k, added in their order.
+template <class T>
+__global__ __launch_bounds__(kBlock) void k_parts(const PartsArgs a)
+{
+    const uint32_t p = blockIdx.x * kBlock + threadIdx.x, row = p / a.packs, c = (p - row * a.packs) * 8;
+    if (row >= a.rows) return;
+    const float *from = a.parts + (int64_t)row * a.ld + c;
+    Eight sum = load_eight<ElemF32>(from, 8);         // (rows of the ranges are whole packs)
+    for (int i = 1; i < a.count; i++) {
+        const Eight v = load_eight<ElemF32>(from + i * a.part, 8);
+#pragma unroll
+        for (int e = 0; e < 8; e++) sum.v[e] += v.v[e];
+    }
+    store_eight<T>((typename T::elem *)a.y + (int64_t)row * a.ldy + c, sum, a.width - (int)c);
+}
+
+template <class T>
+int run_parts(const PartsArgs &a, hipStream_t st)
+{
+    k_parts<T><<<cdiv((uint64_t)a.rows * a.packs, kBlock), kBlock, 0, st>>>(a);
+    return launched();
+}
+
+// Ranges of k that y's product is cut into where its tiles leave most of the chip without work: as many as fill it, of 512 k at
+// least.  Not in training: how many there are goes by the batch, and with them the bits that a file's gradient is made from.
+int forward_parts(const ccdc_block_t *b, int64_t rows)
+{
+    const int64_t tiles = (int64_t)cdiv(b->c.width, 128) * cdiv(rows, 128);
+    return tiles > 128 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, b->hidden_ld / 512));
+}
+
 // What every product of the block is given.
 ProductArgs common(const ccdc_block_t *b)
 {
@@ -117,8 +156,19 @@ int forward(const ccdc_block_t *b, int64_t rows, const void *x, int64_t ldx, con
     a = common(b);
     a.n = out, a.m = hidden_side(b, h);
     a.rows_n = (int32_t)d, a.rows_m = (int32_t)rows, a.K = (int32_t)padded(F);
-    a.c = y, a.ldc = ldy;
-    return run_product(b->c.mode, Product::plain, a, st);
+    const int parts = saved ? 1 : forward_parts(b, rows);
+    if (parts == 1) {
+        a.c = y, a.ldc = ldy;
+        return run_product(b->c.mode, Product::plain, a, st);
+    }
+    float *made = inside_of<float>(b->d_workspace, b->at_parts);
+    const int64_t steps = (padded(F) + 63) / 64;
+    a.part_k = (int32_t)((steps + parts - 1) / parts * 64);
+    a.files = (int32_t)cdiv(padded(F), a.part_k);
+    a.c = made, a.ldc = b->width_ld, a.file_c = rows * b->width_ld;
+    if ((rc = run_product(b->c.mode, Product::parts, a, st)) != CCDC_OK) return rc;
+    const PartsArgs p{made, y, a.file_c, a.ldc, ldy, a.files, (int32_t)d, (uint32_t)rows, (uint32_t)(b->width_ld / 8)};
+    CCDC_BY_ELEM(b, (run_parts<T>(p, st)));
 }
 
 int backward(const ccdc_block_t *b, const void *x, int64_t ldx, const void *W_in, const void *W_out, const void *saved, const void *dy,

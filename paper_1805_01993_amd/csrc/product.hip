@@ -139,7 +139,7 @@ __device__ __forceinline__ Bits8 piece(CCDC_LDS unsigned char *lds, int row0, in
 template <class T, Product WHAT, int WN, int WM, int SN, int SM, int BUFFERS>
 __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
 {
-    constexpr bool NS = WHAT != Product::gated && WHAT != Product::plain, MS = WHAT == Product::weight_gradient;
+    constexpr bool NS = WHAT != Product::gated && WHAT != Product::plain && WHAT != Product::parts, MS = WHAT == Product::weight_gradient;
     constexpr bool GATED = WHAT == Product::gated;
     constexpr int THREADS = 64 * WN * WM, TN = WN * SN * 32, TM = WM * SM * 32;
     // fp32: a step has all planes of 32 k, so that each is copied and read once for the products that it is in
@@ -166,6 +166,13 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
         K = a.first[file + 1] - from;
         sn.p += from * sn.ld;
         sm.p += from * sm.ld + half * sm.segment;
+    }
+    if constexpr (WHAT == Product::parts) {
+        file = product;
+        const int64_t from = (int64_t)file * a.part_k;
+        K = (int32_t)min(a.K - from, (int64_t)a.part_k);
+        sn.p += from;
+        sm.p += from;
     }
     Copies<NS, TN, THREADS, STEP> cn;
     Copies<MS, TM, THREADS, STEP> cm;
@@ -347,7 +354,8 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
     // The result goes through LDS, a wavefront's rows of 64 n at a time, each by itself: an accumulator's lanes have four n of 32 rows,
     // a store of which would be 32 pieces of as many lines; after it eight lanes have a row's 64.
     static_assert(SN == 2);
-    using E = typename T::elem;
+    using Result = std::conditional_t<WHAT == Product::parts, ElemF32, T>;
+    using E = typename Result::elem;
     constexpr bool NARROW = sizeof(E) == 2 && WHAT != Product::gated && WHAT != Product::gated_gradient;      // staged as stored
 #pragma unroll
     for (int j = 0; j < SM; j++) {
@@ -443,7 +451,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
                                 if (e < valid) to[e] = (E)v[e];
                         }
                     } else {
-                        store_eight<T>(to, staged(row, pack), a.rows_n - n);
+                        store_eight<Result>(to, staged(row, pack), a.rows_n - n);
                     }
                 }
             }
@@ -483,6 +491,8 @@ int by_tile(const ProductArgs &a, hipStream_t st)
 {
     if constexpr (T::planes == 3) {
         return launch<T, WHAT, 2, 4, 2, 1, 3>(a, st);
+    } else if constexpr (WHAT == Product::parts) {
+        return launch<T, WHAT, 2, 4, 2, 1, 4>(a, st);
     } else {
         if (large_tiles<WHAT>(a)) return launch<T, WHAT, 4, 2, 2, 4, 2>(a, st);
         const uint64_t small = (uint64_t)cdiv(a.rows_n, WHAT == Product::gated ? 64 : 128) * cdiv(a.rows_m, 128) * a.files * a.halves;
@@ -497,6 +507,7 @@ int by_product(Product what, const ProductArgs &a, hipStream_t st)
     switch (what) {
     case Product::gated: return by_tile<T, Product::gated>(a, st);
     case Product::plain: return by_tile<T, Product::plain>(a, st);
+    case Product::parts: return by_tile<T, Product::parts>(a, st);
     case Product::gated_gradient: return by_tile<T, Product::gated_gradient>(a, st);
     case Product::input_gradient: return by_tile<T, Product::input_gradient>(a, st);
     default: return by_tile<T, Product::weight_gradient>(a, st);

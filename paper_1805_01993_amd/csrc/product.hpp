@@ -18,6 +18,7 @@ struct Side {
 enum class Product {
     gated,                        // N: W_in, M: x.  h (and what the backward needs) from a and u
     plain,                        // N: W_out, M: h.  y
+    parts,                        // the same in ranges of k, a product each, in fp32: what k_parts adds up
     gated_gradient,               // N: W_out strided, M: dy.  gradients of a and u from that of h
     input_gradient,               // N: W_in strided, M: gradients of a and u.  dx
     weight_gradient               // both strided, a product per file: dW_in, dW_out
@@ -29,6 +30,7 @@ struct ProductArgs {
     int32_t K, segments;          // weight_gradient: the files' tokens on average, for the choice of a tile
     int32_t tiles_n, tiles_m;
     const int32_t *first;         // weight_gradient: rows of k where the files begin
+    int32_t part_k;               // parts: k of a range, whole steps; files is their number
     int32_t files, halves;        // halves: products a file has, side M of the second from its segment on
     void *c;                      // result
     int64_t ldc, file_c, half_c;

@@ -131,6 +131,14 @@ def test_ffn_few_rows(torch, L, mode, rows, d, F):
 
 
 @pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("rows,d,F", [(65, 264, 2060), (130, 72, 4096), (300, 515, 1333), (129, 1000, 1536), (66, 9, 5000)])
+def test_ffn_rows_that_leave_the_chip_without_work(torch, L, mode, rows, d, F):
+    """The second product in ranges of its k, whole and not, that are added up."""
+    got, want = run_ffn(torch, L, [rows], d, F, mode, train=False)
+    close("y", got["y"], want["y"])
+
+
+@pytest.mark.parametrize("mode", MODES)
 def test_ffn_large_tiles(torch, L, mode):
     """Enough tiles of 256 x 256 for those kernels, sizes that end inside one."""
     got, want = run_ffn(torch, L, [1100, 0, 963], 1048, 3992, mode, p=0.1)
