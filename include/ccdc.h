@@ -323,7 +323,8 @@ int ccdc_node_decode_reduce(const ccdc_plan_t *plan, int node, const void *V, co
  * Elements are those of the mode (fp32 for CCDC_F32_SUM and CCDC_F32_SUM_XOR, bfloat16, binary16); CCDC_U32_XOR
  * has no products and is refused.  Sums, norms and activations are carried in fp32; results are rounded once, to
  * nearest even.  In the 16-bit modes h and the gradients of a and u are rounded to the mode's format between the
- * products that make and those that take them; in fp32 the products are exact to 2^-24 or so.
+ * products that make and those that take them; in fp32 the products are exact to 2^-24 or so (of an infinite
+ * operand they make NaN).
  * Matrices are row-major with a row stride in elements (ld...), at least their width, columns contiguous; any
  * alignment to the element is taken.
  */
@@ -375,7 +376,8 @@ int ccdc_block_query(const ccdc_block_t *block, int what, void *out, size_t out_
  */
 
 /* y [rows][width] from x [rows][width].  saved: NULL, or CCDC_BLOCK_Q_SAVED_BYTES bytes, aligned to 16, for the
- * backward call (then rows must be M). */
+ * backward call (then rows must be M).  Without it, calls of a few rows or hundreds take kernels of their own, whose
+ * sums have another order. */
 int ccdc_ffn_forward(const ccdc_block_t *block, int64_t rows, const void *x, int64_t ldx, const void *W_in,
                      const void *W_out, void *y, int64_t ldy, void *saved, uint64_t seed, void *stream);
 
@@ -388,7 +390,7 @@ int ccdc_ffn_backward(const ccdc_block_t *block, const void *x, int64_t ldx, con
 
 /* The join.  f NULL: y = residual_scale x and no gate; n NULL: without the norm after it; y NULL: only n.  w_post, w_pre NULL: ones;
  * gate NULL: one, else [width], the same for every file (ld_gate 0), or a row per file (ld_gate >= width).
- * All matrices have row stride ld.  y may be x or f; n may be x or f. */
+ * All matrices have row stride ld.  y may be x or f; n may be x or f.  CCDC_ESIZE for a width above 16384. */
 int ccdc_join_forward(const ccdc_block_t *block, int64_t rows, const void *x, const void *f, const void *w_post,
                       const void *gate, int64_t ld_gate, const void *w_pre, void *y, void *n, int64_t ld,
                       uint64_t seed, void *stream);
@@ -396,7 +398,8 @@ int ccdc_join_forward(const ccdc_block_t *block, int64_t rows, const void *x, co
 /* From dn, the gradient of n (NULL: there is no n), and dr, the gradient that reaches y by other ways (NULL: none;
  * not both NULL): dx and df (NULL with f), and file by file dw_post, dgate, dw_pre (rows of `width` elements, ld_file
  * apart; NULL: not wanted).  y as ccdc_join_forward stored it (needed with dn).  A gate shared by the files has its
- * gradient file by file like everything else.  dx may be dr or dn; df may be f, or dn or dr where dx is not. */
+ * gradient file by file like everything else.  dx may be dr or dn; df may be f, or dn or dr where dx is not.
+ * CCDC_ESIZE as above. */
 int ccdc_join_backward(const ccdc_block_t *block, const void *dn, const void *dr, const void *y, const void *f,
                        const void *w_post, const void *gate, int64_t ld_gate, const void *w_pre, void *dx, void *df,
                        int64_t ld, void *dw_post, void *dgate, void *dw_pre, int64_t ld_file, uint64_t seed,

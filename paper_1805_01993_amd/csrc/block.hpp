@@ -19,8 +19,8 @@ struct RowOf {
 struct Chunk {
     int32_t file, first, rows;
 };
-// 32 rows of 2048 bf16 values are four wavefronts' work for some 25 us; the sums of a chunk, written and read once
-// more, are 4 % of what its rows move.  The same for every batch: the order of a file's sums is its own.
+// The same for every batch: the order of a file's sums is its own.  The sums of a chunk, written and read once more, are 4 % of what 32
+// rows of bf16 values move; chunks of 16 took 0.99 of the time (14336 x 2048 bf16).
 constexpr int kChunkRows = 32;
 constexpr int64_t kJoinWidth = 16384;         // widest rows that one workgroup holds in registers
 
@@ -56,7 +56,7 @@ struct ccdc_block_s {
     int32_t *d_first = nullptr, *d_chunk_first = nullptr;
     ccdc::RowOf *d_row_of = nullptr;
     ccdc::Chunk *d_chunks = nullptr;
-    void *d_workspace = nullptr;
+    void *d_tables = nullptr, *d_workspace = nullptr;       // d_first .. d_chunks are parts of the first
 
     // as a plan's (plan.hpp)
     mutable std::mutex ws_mutex;

@@ -42,6 +42,26 @@ __device__ __forceinline__ V fresh_uniform(V v)
 // 1 for the first `valid` of a pack's elements, else 0, without a mask.
 __device__ __forceinline__ int inside(int valid, int i) { return min(max(valid - i, 0), 1); }
 
+// Rounded to nearest even.  Unlike a payload's sums (Hyb16::narrow) a NaN keeps what the conversion makes of it: two instructions an
+// element less.
+template <class T>
+__device__ __forceinline__ typename T::elem narrow(float x)
+{
+    if constexpr (sizeof(typename T::elem) == 2) {
+        typename T::elem out;
+        if constexpr (std::is_base_of<HybBF16, T>::value) {
+            const __bf16 h = (__bf16)x;
+            __builtin_memcpy(&out, &h, 2);
+        } else {
+            const _Float16 h = (_Float16)x;
+            __builtin_memcpy(&out, &h, 2);
+        }
+        return out;
+    } else {
+        return x;
+    }
+}
+
 // As loaded; zeros past the row's end.
 template <class T>
 struct Raw8 {
@@ -101,13 +121,13 @@ __device__ __forceinline__ void store_eight(typename T::elem *p, const Eight &x,
         for (int h = 0; h < 8 / W; h++) {
             P q;
 #pragma unroll
-            for (int i = 0; i < W; i++) q.v[i] = T::narrow(x.v[h * W + i]);
+            for (int i = 0; i < W; i++) q.v[i] = narrow<T>(x.v[h * W + i]);
             store_at<STREAM, true, P, E>(p + h * W, q);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (i < valid) p[i] = T::narrow(x.v[i]);
+            if (i < valid) p[i] = narrow<T>(x.v[i]);
     }
 }
 
@@ -125,8 +145,11 @@ inline Dropout make_dropout(double p, uint32_t site, uint64_t seed)
     return {{(uint32_t)seed, (uint32_t)(seed >> 32)}, site, t, t >= 65536 ? 0.0f : 65536.0f / (float)(65536 - t)};
 }
 
-// The factors of columns 8 * unit .. 8 * unit + 7 of a row.
-__device__ __forceinline__ Eight dropout_factors(const Dropout &d, uint32_t id, uint32_t token, uint32_t unit)
+// The random numbers of columns 8 * unit .. 8 * unit + 7 of a row, two a word.
+struct Words {
+    uint32_t w[4];
+};
+__device__ __forceinline__ Words dropout_words(const Dropout &d, uint32_t id, uint32_t token, uint32_t unit)
 {
     uint32_t c0 = unit, c1 = token, c2 = id, c3 = d.site, k0 = d.key[0], k1 = d.key[1];
 #pragma unroll
@@ -139,10 +162,25 @@ __device__ __forceinline__ Eight dropout_factors(const Dropout &d, uint32_t id, 
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
-    const uint32_t w[4] = {c0, c1, c2, c3};
+    return {{c0, c1, c2, c3}};
+}
+__device__ __forceinline__ uint32_t half_of(const Words &r, int i) { return i % 2 ? r.w[i / 2] >> 16 : r.w[i / 2] & 0xFFFFu; }
+
+// Takes out of eight values what dropout takes out (an infinity or no number too), and multiplies the others.
+__device__ __forceinline__ void drop_eight(Eight &v, const Dropout &d, uint32_t id, uint32_t token, uint32_t unit)
+{
+    const Words r = dropout_words(d, id, token, unit);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v.v[i] = half_of(r, i) >= d.threshold ? v.v[i] * d.scale : 0.0f;
+}
+
+// The same as factors, 0 for what is taken out.
+__device__ __forceinline__ Eight dropout_factors(const Dropout &d, uint32_t id, uint32_t token, uint32_t unit)
+{
+    const Words r = dropout_words(d, id, token, unit);
     Eight f;
 #pragma unroll
-    for (int i = 0; i < 8; i++) f.v[i] = (i % 2 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu) >= d.threshold ? d.scale : 0.0f;
+    for (int i = 0; i < 8; i++) f.v[i] = half_of(r, i) >= d.threshold ? d.scale : 0.0f;
     return f;
 }
 

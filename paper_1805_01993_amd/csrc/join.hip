@@ -8,7 +8,8 @@ using namespace ccdc;
 
 constexpr int kJoinWaves = 4;         // wavefronts of a workgroup where a row has fewer
 // Rows that a workgroup of the gradient has at a time.  A row is a chain of four sums over it and three waits for memory, 9 us of them
-// at 2048 columns, so a chunk's rows go several abreast: 14336 x 2048 bf16 one at a time 298 us.
+// at 2048 columns, so a chunk's rows go several abreast: 14336 x 2048 bf16 one at a time 298 us, four 117 (3.0 TB/s); 14348 x 1001 fp32
+// four at a time 117 us, eight 86.
 constexpr int teams(int waves) { return waves < 8 ? 8 / waves : 1; }
 
 struct JoinArgs {
@@ -219,9 +220,7 @@ __device__ __forceinline__ void drop(Share<WAVES, PACKS> &v, const Dropout &d, c
     for (int i = 0; i < PACKS; i++) {
         const int unit = pack_of<WAVES>(i);
         if (unit * 8 >= width) continue;
-        const Eight k = dropout_factors(d, row.id, row.token, unit);
-#pragma unroll
-        for (int e = 0; e < 8; e++) v.p[i].v[e] = kept(v.p[i].v[e], k.v[e]);
+        drop_eight(v.p[i], d, row.id, row.token, unit);
     }
 }
 
@@ -336,11 +335,7 @@ __global__ __launch_bounds__(64 * WAVES * teams(WAVES)) void k_join_gradient(con
 #pragma unroll
             for (int i = 0; i < PACKS; i++) {
                 const int unit = fresh(pack_of<WAVES>(i));
-                if (drop.threshold && unit * 8 < width) {
-                    const Eight f = dropout_factors(drop, of.id, of.token, unit);
-#pragma unroll
-                    for (int k = 0; k < 8; k++) dy.p[i].v[k] = kept(dy.p[i].v[k], f.v[k]);
-                }
+                if (drop.threshold && unit * 8 < width) drop_eight(dy.p[i], drop, of.id, of.token, unit);
                 if (own)
 #pragma unroll
                     for (int k = 0; k < 8; k++) sum_at(0, i, k) += dy.p[i].v[k] * hat.p[i].v[k];
@@ -408,11 +403,11 @@ __global__ __launch_bounds__(kBlock) void k_learned(const LearnedArgs a)
     for (; k < end; k++) v[0] += p[k * step];
     const float sum = (v[0] + v[1]) + (v[2] + v[3]);
     if (which == 1) {
-        ((E *)a.w_pre)[at] = T::narrow(sum);
+        ((E *)a.w_pre)[at] = narrow<T>(sum);
         return;
     }
-    if (a.w_post) ((E *)a.w_post)[at] = T::narrow(a.by_gate ? sum * T::widen(((const E *)a.by_gate)[file * a.ld_gate + c]) : sum);
-    if (a.gate) ((E *)a.gate)[at] = T::narrow(a.by_post ? sum * T::widen(((const E *)a.by_post)[c]) : sum);
+    if (a.w_post) ((E *)a.w_post)[at] = narrow<T>(a.by_gate ? sum * T::widen(((const E *)a.by_gate)[file * a.ld_gate + c]) : sum);
+    if (a.gate) ((E *)a.gate)[at] = narrow<T>(a.by_post ? sum * T::widen(((const E *)a.by_post)[c]) : sum);
 }
 
 struct DropoutArgs {
@@ -439,12 +434,10 @@ __global__ __launch_bounds__(kBlock) void k_dropout(const DropoutArgs a)
     Eight v = load_eight<T>((const E *)a.x + (int64_t)row * a.ldx + c, valid), res = {};
     if (a.residual) res = load_eight<T>((const E *)a.residual + (int64_t)row * a.ld_residual + c, valid);
     const RowOf of = a.row_of[row];
-    const Eight k = dropout_factors(a.drop, of.id, of.token, unit);
+    drop_eight(v, a.drop, of.id, of.token, unit);
+    if (a.residual)
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        v.v[i] = kept(v.v[i], k.v[i]);
-        if (a.residual) v.v[i] += res.v[i];
-    }
+        for (int i = 0; i < 8; i++) v.v[i] += res.v[i];
     store_eight<T>((E *)a.y + (int64_t)row * a.ldy + c, v, valid);
 }
 

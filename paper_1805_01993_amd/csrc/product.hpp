@@ -50,12 +50,12 @@ int run_product(int mode, Product what, ProductArgs a, hipStream_t st);
 // largest numbers, where that would be an infinity, cut instead.  Infinities and NaN are their first part.
 __device__ __forceinline__ void split(float x, uint16_t *part)
 {
-    float first = HybBF16::widen(HybBF16::narrow(x));
+    float first = HybBF16::widen(narrow<ElemBF16>(x));
     if (fabsf(first) > 3.4e38f) first = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
     const float left = fabsf(first) <= 3.4e38f ? x - first : 0.0f;
     part[0] = (uint16_t)(__float_as_uint(first) >> 16);
-    part[1] = HybBF16::narrow(left);
-    part[2] = HybBF16::narrow(left - HybBF16::widen(part[1]));
+    part[1] = narrow<ElemBF16>(left);
+    part[2] = narrow<ElemBF16>(left - HybBF16::widen(part[1]));
 }
 
 // Eight numbers as a side of a later product.
