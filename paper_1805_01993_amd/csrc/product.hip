@@ -492,6 +492,12 @@ template <class T, Product WHAT>
 int by_tile(const ProductArgs &a, hipStream_t st)
 {
     if constexpr (T::planes == 3) {
+        // fp32: 128 x 256 or 128 x 128, one a CU; a round of the former has twice the work in 1.45 to 1.7 of the time (4040 tokens,
+        // 1024 x 2600: a and u in 3 rounds 285 us, 6 of small ones 336; dx, whose large tiles are half a round, 416 and 282)
+        const auto rounds = [&](uint32_t m) {
+            return (double)cdiv((uint64_t)cdiv(a.rows_n, WHAT == Product::gated ? 64 : 128) * cdiv(a.rows_m, m) * a.files * a.halves, 256);
+        };
+        if (WHAT != Product::parts && rounds(256) * 1.6 <= rounds(128)) return launch<T, WHAT, 2, 4, 2, 2, 2>(a, st);
         return launch<T, WHAT, 2, 4, 2, 1, 3>(a, st);
     } else if constexpr (WHAT == Product::parts) {
         return launch<T, WHAT, 2, 4, 2, 1, 4>(a, st);
