@@ -42,14 +42,16 @@ int run_sides(const SidesArgs &a, hipStream_t st)
     return launched();
 }
 
-// The caller's matrices as sides of products: as they are where rows of 16-bit numbers are whole packs of 16 bytes, else made
-// in the workspace by one launch.
+constexpr int64_t kSideStride = (int64_t)1 << 24;
+
+// The caller's matrices as sides of products: as they are where rows of 16-bit numbers are whole packs of 16 bytes, no further apart than
+// 64 rows' offsets have bits for, else made in the workspace by one launch.
 class Sides {
 public:
     Sides(const ccdc_block_t *b, hipStream_t st) : b_(b), st_(st) {}
     Side add(const void *p, int64_t ld, int64_t rows, int64_t columns, size_t room)
     {
-        if (b_->planes == 1 && columns % 8 == 0 && ld % 8 == 0 && aligned(p, 16)) return {(const uint16_t *)p, ld, 0, 0, (int32_t)columns};
+        if (b_->planes == 1 && columns % 8 == 0 && ld % 8 == 0 && ld <= kSideStride && aligned(p, 16)) return {(const uint16_t *)p, ld, 0, 0, (int32_t)columns};
         const int64_t wide = padded(columns);
         uint16_t *to = inside_of<uint16_t>(b_->d_workspace, room);
         const uint32_t packs = (uint32_t)(wide / 8);

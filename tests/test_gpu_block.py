@@ -115,6 +115,15 @@ def test_ffn_strides_and_alignment(torch, L, mode, ldx, shift):
         close(name, got[name], want[name])
 
 
+def test_ffn_rows_far_apart(torch, L):
+    """Row strides with which 64 rows are over 2^32 bytes: columns of a matrix of 34 million."""
+    got, want = run_ffn(torch, L, [50, 20], 64, 72, "bf16", ldx=(1 << 25) + 8)
+    for name in got:
+        close(name, got[name].contiguous(), want[name])
+    got, want = run_ffn(torch, L, [9], 64, 72, "bf16", train=False, ldx=(1 << 25) + 8)
+    close("y", got["y"].contiguous(), want["y"])
+
+
 @pytest.mark.parametrize("mode", MODES)
 def test_ffn_everything_dropped(torch, L, mode):
     got, want = run_ffn(torch, L, [9], 32, 48, mode, p=1.0)
