@@ -205,7 +205,8 @@ struct Reader {
             return (void *)fail();
         return t->data_ptr();
     }
-    // Gradients by file, a file's part contiguous; all that are given with one stride.
+    // Gradients by file, a file's part contiguous, no file's on another's; all that are given with one stride (0 in *ld: none yet, which
+    // no stride is).
     void *gradient(PyObject *o, int64_t rows, int64_t columns, int64_t *ld)
     {
         if (o == Py_None) return nullptr;
@@ -214,7 +215,7 @@ struct Reader {
         if (!t || t->dim() != last + 1 || t->size(0) != m.files || t->size(last) != columns || (rows && t->size(1) != rows)) return (void *)fail();
         if ((columns > 1 && t->stride(last) != 1) || (rows > 1 && t->stride(1) != columns)) return (void *)fail();
         if (m.files > 1) {
-            if (*ld && *ld != t->stride(0)) return (void *)fail();
+            if (t->stride(0) < (rows ? rows : 1) * columns || (*ld && *ld != t->stride(0))) return (void *)fail();
             *ld = t->stride(0);
         }
         return t->data_ptr();
