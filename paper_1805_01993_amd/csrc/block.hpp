@@ -1,6 +1,7 @@
 // A trained block (ccdc_block): its configuration, the batch it is bound to, and what its calls share.
 #pragma once
 
+#include <cmath>
 #include <cstddef>
 #include <cstdint>
 #include <mutex>
@@ -67,8 +68,8 @@ struct ccdc_block_s {
 
 namespace ccdc {
 
-// The thresholds of 16-bit random numbers below which dropout takes a value out.
-inline uint32_t dropout_threshold(double p) { return (uint32_t)(p * 65536.0 + 0.5); }
+// The threshold of 16-bit random numbers below which dropout takes a value out: to nearest, ties to even.
+inline uint32_t dropout_threshold(double p) { return (uint32_t)std::rint(p * 65536.0); }
 
 int bind_block(ccdc_block_t *b, int files, const int64_t *tokens, const int32_t *ids);
 
