@@ -60,9 +60,11 @@ class Trainer:
         files = list(files)
         block = ccdc_block(self.width, self.hidden, self.mode, residual_scale=self.scale, dropout_hidden=self.dropout,
                            dropout_out=self.dropout).bind([self.tokens[n] for n in files], files).upload()
+        # the norm of x alone, in front: a join scales what it norms, so this one's scale is one
+        first = ccdc_block(self.width, 1, self.mode).bind([self.tokens[n] for n in files], files).upload()
         rows = block.tokens
         new = lambda: torch.empty(rows, self.width, dtype=self.x.dtype, device="cuda")  # noqa: E731
-        return {"block": block, "saved": torch.empty(block.saved_bytes, dtype=torch.uint8, device="cuda"),
+        return {"block": block, "first": first, "saved": torch.empty(block.saved_bytes, dtype=torch.uint8, device="cuda"),
                 "n": new(), "f": new(), "y": new(), "df": new(), "dn": new()}
 
     def parameters(self):
@@ -80,14 +82,14 @@ class Trainer:
         for name, shape in self.sizes.items():
             grad[name] = rows[:, at:at + math.prod(shape)].unflatten(1, shape)
             at += math.prod(shape)
-        block.join_forward(x, None, None, s["n"], w_pre=p["w_pre"])
+        s["first"].join_forward(x, None, None, s["n"], w_pre=p["w_pre"])
         block.ffn_forward(s["n"], p["W_in"], p["W_out"], s["f"], saved=s["saved"], seed=seed)
         block.join_forward(x, s["f"], s["y"], None, w_post=p["w_post"], gate=p["gate"], seed=seed)
         off = s["y"].float() - target.float()
         block.join_backward(None, off.to(x.dtype), None, s["f"], None, s["df"], w_post=p["w_post"], gate=p["gate"],
                             dw_post=grad["w_post"], dgate=grad["gate"], seed=seed)
         block.ffn_backward(s["n"], p["W_in"], p["W_out"], s["saved"], s["df"], s["dn"], grad["W_in"], grad["W_out"])
-        block.join_backward(s["dn"], None, x, None, None, None, w_pre=p["w_pre"], dw_pre=grad["w_pre"])
+        s["first"].join_backward(s["dn"], None, x, None, None, None, w_pre=p["w_pre"], dw_pre=grad["w_pre"])
         return off.square().mean() / 2
 
     def step(self, number, rate=0.5):
