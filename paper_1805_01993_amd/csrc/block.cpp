@@ -54,8 +54,7 @@ int bind_block(ccdc_block_t *b, int files, const int64_t *tokens, const int32_t 
     for (int n = 0; n < files; n++) {
         const int32_t id = ids ? ids[n] : n, rows = (int32_t)tokens[n];
         for (int32_t t = 0; t < rows; t++) row_of.push_back({id, t, n});
-        for (int32_t t = 0; t < rows; t += kChunkRows)
-            chunks.push_back({n, first[n] + t, rows - t < kChunkRows ? rows - t : kChunkRows});
+        each_chunk(rows, [&](int32_t t, int32_t of) { chunks.push_back({n, first[n] + t, of}); });
         first.push_back(first[n] + rows);
         chunk_first.push_back((int32_t)chunks.size());
         numbers.push_back(id);

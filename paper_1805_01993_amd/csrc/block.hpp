@@ -23,6 +23,14 @@ struct Chunk {
 // The same for every batch: the order of a file's sums is its own.  The sums of a chunk, written and read once more, are 4 % of what 32
 // rows of bf16 values move; chunks of 16 took 0.99 of the time (14336 x 2048 bf16).
 constexpr int kChunkRows = 32;
+
+// f(first row, rows) for the chunks of a file.  (The row after the last may be 2^31.)
+template <class F>
+void each_chunk(int32_t rows, F f)
+{
+    for (int64_t t = 0; t < rows; t += kChunkRows) f((int32_t)t, (int32_t)(rows - t < kChunkRows ? rows - t : kChunkRows));
+}
+
 constexpr int64_t kJoinWidth = 16384;         // widest rows that one workgroup holds in registers
 
 // Elements of y in all ranges of k together where its product is cut into some: those of 256 tiles.

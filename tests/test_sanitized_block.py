@@ -34,3 +34,9 @@ def test_thresholds_of_dropout_go_to_the_nearest_even(sweep):
         ps += [tie, tie * (1 - 2.0 ** -52), tie * (1 + 2.0 ** -52)]
     got = [int(v) for v in sweep("thresholds", *(p.hex() for p in ps)).split()]
     assert got == [round(Fraction(p) * 65536) for p in ps]
+
+
+@pytest.mark.parametrize("rows", [0, 1, 31, 32, 33, 4096, (1 << 31) - 33, (1 << 31) - 32, (1 << 31) - 31, (1 << 31) - 1])
+def test_chunks_of_files_up_to_the_longest(sweep, rows):
+    """Up to the 2^31-1 tokens that a batch may have, where the row after the last chunk is no 32-bit number."""
+    assert int(sweep("chunks", rows)) == -(-rows // 32)
