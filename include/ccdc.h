@@ -318,7 +318,8 @@ int ccdc_node_decode_reduce(const ccdc_plan_t *plan, int node, const void *V, co
  * halfword c % 8 (word (c % 8) / 2, low half first) of Philox4x32-10 (Salmon, Moraes, Dror, Shaw 2011) on the
  * counter (c / 8, t, id, site) and the key (low, high half of seed) is at least thr = rint(65536 p), and
  * multiplied by 65536 / (65536 - thr); thr = 65536 keeps nothing.  site tells apart the masks of one step:
- * 2 layer for h, 2 layer + 1 for a join.  No mask is stored; the gradient calls make it again from the same seed.
+ * 2 layer for h, 2 layer + 1 for a join.  No mask is stored: the gradient calls have it from what was saved, or make it
+ * again from the same seed.  What is taken out counts for nothing there either, whatever its gradient (an infinity, a NaN).
  *
  * Elements are those of the mode (fp32 for CCDC_F32_SUM and CCDC_F32_SUM_XOR, bfloat16, binary16); CCDC_U32_XOR
  * has no products and is refused.  Sums, norms and activations are carried in fp32; results are rounded once, to

@@ -36,6 +36,9 @@ typedef _Float16 Half8 __attribute__((ext_vector_type(8)));
 
 __device__ const uint32_t zeros[4] = {};       // what is read in place of k past the end
 
+// P of a hidden value that dropout took out.
+constexpr float kTakenOut = -0.0f;
+
 template <class T>
 __device__ __forceinline__ Acc multiply(Bits8 n, Bits8 m, Acc c)
 {
@@ -414,7 +417,11 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
                     float value, slope;
                     activate<T>(a.activation, va.v[e], value, slope);
                     h.v[e] = value * vu.v[e], P.v[e] = slope * vu.v[e], Q.v[e] = value;
-                    if (a.drop.threshold) h.v[e] = kept(h.v[e], keep.v[e]), P.v[e] = kept(P.v[e], keep.v[e]), Q.v[e] = kept(Q.v[e], keep.v[e]);
+                    P.v[e] += 0.0f;           // (no negative zero: that is what is taken out)
+                    if (a.drop.threshold) {
+                        h.v[e] = kept(h.v[e], keep.v[e]), Q.v[e] = kept(Q.v[e], keep.v[e]);
+                        P.v[e] = keep.v[e] != 0.0f ? P.v[e] * keep.v[e] : kTakenOut;
+                    }
                     if (f + e >= a.rows_n) h.v[e] = P.v[e] = Q.v[e] = 0.0f;
                 }
                 const int64_t at = (int64_t)m * a.ldh + f;
@@ -433,8 +440,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
                     Eight da, du;
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
-                        da.v[e] = v.v[e] * P.v[e], du.v[e] = v.v[e] * Q.v[e];
-                        if (n + e >= a.rows_n) da.v[e] = du.v[e] = 0.0f;
+                        // nothing comes of a value that was taken out, whatever its gradient (an infinity or no number too)
+                        const bool none = n + e >= a.rows_n || __float_as_uint(P.v[e]) == __float_as_uint(kTakenOut);
+                        da.v[e] = none ? 0.0f : v.v[e] * P.v[e], du.v[e] = none ? 0.0f : v.v[e] * Q.v[e];
                     }
                     uint16_t *to = a.h + (int64_t)m * 2 * a.ldh + n;
                     store_side<T>(to, a.plane_h, da);

@@ -37,7 +37,7 @@ struct ProductArgs {
     // gated, gated_gradient: matrices of the hidden values
     uint16_t *h;                  // gated: h; gated_gradient: gradient of a, of u from h_second on
     int64_t ldh, plane_h, second_h;
-    float *P, *Q;                 // gradient of h to those of a and u, [rows_m][ldh]; gated: null: not wanted
+    float *P, *Q;                 // gradient of h to those of a and u, [rows_m][ldh], P -0 where both are 0; gated: null: not wanted
     const RowOf *row_of;
     Dropout drop;
     int32_t activation;

@@ -31,3 +31,35 @@ def test_dropout_at_ties(torch, L, ties):  # noqa: F811
     one = np.ones(d)
     close("z", z, R.join(xv, xv, one, one, one, R.factors(lengths, [0], d, thr / 65536, 9, SEED), 1.0, float(np.float32(1e-6)), False,
                          "f32")["y"])
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("d,F,rows", [(64, 200, 40), (51, 133, 70)])
+def test_what_dropout_takes_out_counts_for_nothing_in_the_gradients(torch, L, mode, act, bad, d, F, rows):  # noqa: F811
+    """One token whose gradient is no finite number: hidden values that were taken out of it have gradients of zero, so their rows of
+    dW_in are what they are with a gradient of zeros there.  Those that were kept are as bad as it."""
+    rng = np.random.default_rng(d)
+    at = 17
+    block = L.ccdc_block(d, F, mode, activation=act, dropout_hidden=0.4, layer=3).bind([rows, 5]).upload()
+    x, _ = numbers(torch, mode, rng, (rows + 5, d))
+    W_in, _ = numbers(torch, mode, rng, (2 * F, d), 1 / np.sqrt(d))
+    W_out, _ = numbers(torch, mode, rng, (d, F), 1 / np.sqrt(F))
+    dy, _ = numbers(torch, mode, rng, (rows + 5, d), 0.25)
+    y, saved = torch.empty_like(x), torch.empty(block.saved_bytes, dtype=torch.uint8, device="cuda")
+    block.ffn_forward(x, W_in, W_out, y, saved=saved, seed=SEED)
+    got = []
+    for v in (0.0, bad):
+        dy[at] = v
+        dx, dW_in, dW_out = torch.empty_like(x), empty(torch, x, 2, 2 * F, d), empty(torch, x, 2, d, F)
+        block.ffn_backward(x, W_in, W_out, saved, dy, dx, dW_in, dW_out)
+        torch.cuda.synchronize()
+        assert torch.isfinite(torch.cat((dx[:at], dx[at + 1:])).float()).all()
+        got.append(dW_in)
+    assert torch.isfinite(got[0].float()).all() and torch.equal(got[0][1], got[1][1])
+    out = torch.from_numpy(R.factors([rows, 5], [0, 1], F, float(np.float32(0.4)), 6, SEED)[at] == 0).cuda()
+    for half in (0, 1):                                # rows of Wg, of Wu
+        zeros, wrong = (g[0, half * F:half * F + F] for g in got)
+        assert torch.equal(zeros[out], wrong[out])
+        assert not torch.isfinite(wrong[~out].float()).any(1).any()
