@@ -400,6 +400,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
         constexpr int LANES = GATED ? 4 : 8;              // that have a row: 32 of a and of u, or 64
 #pragma unroll
         for (int q = 0; q < 32 * LANES / 64; q++) {
+            CCDC_AS_WRITTEN
             const uint32_t row = q * (64 / LANES) + lane / LANES, pack = lane % LANES;
             const int32_t m = tile_m + wm + j * 32 + row;
             if (m >= a.rows_m) continue;

@@ -46,10 +46,15 @@ struct ProductArgs {
 // Launches a product of the mode (ccdc_mode); chooses the tile.
 int run_product(int mode, Product what, ProductArgs a, hipStream_t st);
 
+// What follows a product is in kernels of several tiles, of which one file's values may come from one and on another node from another:
+// with the same operations in each, none that the compiler has put together (a product and a sum in one rounding) in one of them only.
+#define CCDC_AS_WRITTEN _Pragma("clang fp contract(off)")
+
 // The three bfloat16 numbers of an fp32 number.  Rounded to nearest, so that what is left is at most 2^-9 of it; near the
 // largest numbers, where that would be an infinity, cut instead.  Infinities and NaN are their first part.
 __device__ __forceinline__ void split(float x, uint16_t *part)
 {
+    CCDC_AS_WRITTEN
     float first = HybBF16::widen(narrow<ElemBF16>(x));
     if (fabsf(first) > 3.4e38f) first = __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
     const float left = fabsf(first) <= 3.4e38f ? x - first : 0.0f;
@@ -82,14 +87,15 @@ __device__ __forceinline__ void store_side(uint16_t *p, int64_t plane, const Eig
 template <class T>
 __device__ __forceinline__ void activate(int which, float a, float &value, float &slope)
 {
+    CCDC_AS_WRITTEN
     if (which == CCDC_ACT_SILU) {
         const float e = T::planes == 1 ? __expf(-a) : expf(-a), s = 1.0f / (1.0f + e);
         value = a * s;
-        slope = s * (1.0f + a * (1.0f - s));
+        slope = s * fmaf(a, 1.0f - s, 1.0f);
     } else if (which == CCDC_ACT_GELU) {
         const float cdf = 0.5f * (1.0f + erff(a * 0.70710678f));
         value = a * cdf;
-        slope = cdf + a * 0.39894228f * (T::planes == 1 ? __expf(-0.5f * a * a) : expf(-0.5f * a * a));
+        slope = fmaf(a * 0.39894228f, T::planes == 1 ? __expf(-0.5f * a * a) : expf(-0.5f * a * a), cdf);
     } else {
         value = a > 0.0f ? a : a != a ? a : 0.0f;
         slope = a > 0.0f ? 1.0f : 0.0f;

@@ -63,3 +63,36 @@ def test_what_dropout_takes_out_counts_for_nothing_in_the_gradients(torch, L, mo
         zeros, wrong = (g[0, half * F:half * F + F] for g in got)
         assert torch.equal(zeros[out], wrong[out])
         assert not torch.isfinite(wrong[~out].float()).any(1).any()
+
+
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+def test_gradients_are_the_same_in_every_batch_with_every_activation(torch, L, mode, act):  # noqa: F811
+    """Alone and among files that make the products take larger tiles, which are kernels of their own: the same bits of y, dx and
+    the weights' gradients."""
+    rng = np.random.default_rng(12)
+    d, F, lengths = 264, 2060, [70, 513, 1, 300, 640, 129, 700, 650]
+    at = np.concatenate(([0], np.cumsum(lengths)))
+    x, _ = numbers(torch, mode, rng, (sum(lengths), d))
+    dy, _ = numbers(torch, mode, rng, (sum(lengths), d), 0.1)
+    W_in, _ = numbers(torch, mode, rng, (2 * F, d), 1 / 4)
+    W_out, _ = numbers(torch, mode, rng, (d, F), 1 / 45)
+
+    def results(files):
+        block = L.ccdc_block(d, F, mode, activation=act, dropout_hidden=0.15, layer=1).bind([lengths[n] for n in files], files).upload()
+        rows = torch.from_numpy(np.concatenate([np.arange(at[n], at[n + 1]) for n in files])).cuda()
+        px, pdy = x[rows].contiguous(), dy[rows].contiguous()
+        saved = torch.empty(block.saved_bytes, dtype=torch.uint8, device="cuda")
+        y, dx = torch.empty_like(px), torch.empty_like(px)
+        dW_in, dW_out = empty(torch, x, len(files), 2 * F, d), empty(torch, x, len(files), d, F)
+        block.ffn_forward(px, W_in, W_out, y, saved=saved, seed=SEED)
+        block.ffn_backward(px, W_in, W_out, saved, pdy, dx, dW_in, dW_out)
+        torch.cuda.synchronize()
+        by_file = lambda t: torch.split(t, [lengths[n] for n in files])  # noqa: E731
+        return {n: (a, b, dW_in[i], dW_out[i]) for i, (n, a, b) in enumerate(zip(files, by_file(y), by_file(dx)))}
+
+    everything = results(list(range(8)))
+    for files in ([5, 0, 2], [3], [4, 6, 1], [7]):
+        for n, parts in results(files).items():
+            for name, a, b in zip(("y", "dx", "dW_in", "dW_out"), parts, everything[n]):
+                assert torch.equal(a, b), f"file {n} in {files}: {name} differs"
