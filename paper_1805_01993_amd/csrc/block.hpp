@@ -1,6 +1,7 @@
 // A trained block (ccdc_block): its configuration, the batch it is bound to, and what its calls share.
 #pragma once
 
+#include <algorithm>
 #include <cmath>
 #include <cstddef>
 #include <cstdint>
@@ -35,6 +36,14 @@ constexpr int64_t kJoinWidth = 16384;         // widest rows that one workgroup 
 
 // Elements of y in all ranges of k together where its product is cut into some: those of 256 tiles.
 constexpr int64_t kPartElements = (int64_t)256 * 128 * 128;
+
+// Ranges of k that y's product is cut into where its tiles leave most of the chip without work: as many as fill it, of 512 k at
+// least.  Not in training: how many there are goes by the batch's rows, and with them the bits that a file's gradient is made from.
+inline int forward_parts(int64_t width, int64_t hidden_ld, int64_t rows)
+{
+    const int64_t tiles = (width + 127) / 128 * ((rows + 127) / 128);
+    return tiles > 128 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, hidden_ld / 512));
+}
 
 constexpr int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
 

@@ -1,6 +1,4 @@
 // The gated feed-forward block, forward and backward: what is launched, and in which order.
-#include <algorithm>
-
 #include "product.hpp"
 
 namespace {
@@ -107,14 +105,6 @@ int run_parts(const PartsArgs &a, hipStream_t st)
     return launched();
 }
 
-// Ranges of k that y's product is cut into where its tiles leave most of the chip without work: as many as fill it, of 512 k at
-// least.  Not in training: how many there are goes by the batch, and with them the bits that a file's gradient is made from.
-int forward_parts(const ccdc_block_t *b, int64_t rows)
-{
-    const int64_t tiles = (int64_t)cdiv(b->c.width, 128) * cdiv(rows, 128);
-    return tiles > 128 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, b->hidden_ld / 512));
-}
-
 // What every product of the block is given.
 ProductArgs common(const ccdc_block_t *b)
 {
@@ -158,7 +148,7 @@ int forward(const ccdc_block_t *b, int64_t rows, const void *x, int64_t ldx, con
     a = common(b);
     a.n = out, a.m = hidden_side(b, h);
     a.rows_n = (int32_t)d, a.rows_m = (int32_t)rows, a.K = (int32_t)padded(F);
-    const int parts = saved ? 1 : forward_parts(b, rows);
+    const int parts = saved ? 1 : forward_parts(d, b->hidden_ld, rows);
     if (parts == 1) {
         a.c = y, a.ldc = ldy;
         return run_product(b->c.mode, Product::plain, a, st);

@@ -40,3 +40,8 @@ def test_thresholds_of_dropout_go_to_the_nearest_even(sweep):
 def test_chunks_of_files_up_to_the_longest(sweep, rows):
     """Up to the 2^31-1 tokens that a batch may have, where the row after the last chunk is no 32-bit number."""
     assert int(sweep("chunks", rows)) == -(-rows // 32)
+
+
+def test_tables_and_regions_of_batches(sweep):
+    """csrc/block.cpp over configurations and batches: its tables, and that what is saved and the workspace hold what the calls index."""
+    assert int(sweep("batches").removeprefix("clean: ")) == 4 * 12 * 7 * 10
