@@ -47,7 +47,7 @@ int bind_block(ccdc_block_t *b, int files, const int64_t *tokens, const int32_t 
         hidden_ld * width_ld * 2 * operand > kMostBytes)
         return CCDC_ESIZE;
 
-    std::vector<int32_t> first(1, 0), chunk_first(1, 0), numbers;
+    std::vector<int32_t> first(1, 0), chunk_first(1, 0);
     std::vector<RowOf> row_of;
     std::vector<Chunk> chunks;
     row_of.reserve((size_t)M);
@@ -57,7 +57,6 @@ int bind_block(ccdc_block_t *b, int files, const int64_t *tokens, const int32_t 
         each_chunk(rows, [&](int32_t t, int32_t of) { chunks.push_back({n, first[n] + t, of}); });
         first.push_back(first[n] + rows);
         chunk_first.push_back((int32_t)chunks.size());
-        numbers.push_back(id);
     }
 
     size_t at = 0;
@@ -82,7 +81,6 @@ int bind_block(ccdc_block_t *b, int files, const int64_t *tokens, const int32_t 
     b->width_ld = width_ld;
     b->hidden_ld = hidden_ld;
     b->first = std::move(first);
-    b->ids = std::move(numbers);
     b->row_of = std::move(row_of);
     b->chunks = std::move(chunks);
     b->chunk_first = std::move(chunk_first);

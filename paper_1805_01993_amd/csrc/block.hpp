@@ -59,7 +59,6 @@ struct ccdc_block_s {
     int N = 0;
     int64_t hidden_ld = 0, width_ld = 0;          // row strides of the block's own matrices: whole packs of 16 bytes
     std::vector<int32_t> first;       // [N + 1] rows the files begin at
-    std::vector<int32_t> ids;         // [N]
     std::vector<ccdc::RowOf> row_of;  // [M]
     std::vector<ccdc::Chunk> chunks;
     std::vector<int32_t> chunk_first; // [N + 1]

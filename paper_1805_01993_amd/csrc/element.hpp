@@ -109,7 +109,7 @@ __device__ __forceinline__ Eight load_eight(const typename T::elem *p, int valid
     return widen(load_raw<T>(p, valid));
 }
 
-template <class T, bool STREAM = false>
+template <class T>
 __device__ __forceinline__ void store_eight(typename T::elem *p, const Eight &x, int valid)
 {
     using E = typename T::elem;
@@ -122,7 +122,7 @@ __device__ __forceinline__ void store_eight(typename T::elem *p, const Eight &x,
             P q;
 #pragma unroll
             for (int i = 0; i < W; i++) q.v[i] = narrow<T>(x.v[h * W + i]);
-            store_at<STREAM, true, P, E>(p + h * W, q);
+            store_any<P, E>(p + h * W, q);
         }
     } else {
 #pragma unroll
