@@ -324,8 +324,8 @@ int ccdc_node_decode_reduce(const ccdc_plan_t *plan, int node, const void *V, co
  * Elements are those of the mode (fp32 for CCDC_F32_SUM and CCDC_F32_SUM_XOR, bfloat16, binary16); CCDC_U32_XOR
  * has no products and is refused.  Sums, norms and activations are carried in fp32; results are rounded once, to
  * nearest even.  In the 16-bit modes h and the gradients of a and u are rounded to the mode's format between the
- * products that make and those that take them; in fp32 the products are exact to 2^-24 or so (of an infinite
- * operand they make NaN).
+ * products that make and those that take them (binary16: an infinity above 65504); in fp32 the products are exact to
+ * 2^-24 or so (of an infinite operand they make NaN).
  * Matrices are row-major with a row stride in elements (ld...), at least their width, columns contiguous; any
  * alignment to the element is taken.
  */

@@ -1,6 +1,8 @@
 // The feed-forward block for a few rows: an answer's next tokens.  The time is that of reading the weights once, so they go from
 // memory to the matrix instructions' registers without a stop in LDS, as many loads in flight as the chip has room for.
 //
+// h is rounded to the block's elements between the two products, as in product.hip.
+//
 // A wavefront multiplies 16 x 16 pieces by v_mfma_f32_16x16x32, rows of the weights as the instruction's rows.  Its 16 rows are 16 / S
 // rows of the weights in S parts of their k, and its 16 columns as many rows of x in the same S parts: the products of equal
 // parts are what is wanted, the others come for nothing.  With few rows of x that makes a workgroup's share of the weights

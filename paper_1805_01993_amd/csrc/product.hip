@@ -194,7 +194,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0.0f;
 
-    // steps: planes of either side, then ranges of k, then k
+    // steps: k, then ranges of k; each has all planes of either side
     const int32_t in_k = (K + STEP - 1) / STEP, steps = in_k * a.segments;
     // What is copied next of a side: its place in the side's order of steps.
     struct Next {
@@ -426,6 +426,9 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product(const ProductArgs a)
                     if (f + e >= a.rows_n) h.v[e] = P.v[e] = Q.v[e] = 0.0f;
                 }
                 const int64_t at = (int64_t)m * a.ldh + f;
+                // 16-bit modes: rounded to the mode's format, as the gradients of a and u are, since that is what the matrix
+                // instructions multiply (in parts, as fp32 has it, three or six times the products).  Results are 1.4 times as far
+                // off as by their own rounding alone; binary16 has an infinity above 65504.
                 store_side<T>(a.h + at, a.plane_h, h);
                 if (a.P) {
                     store_eight<ElemF32>(a.P + at, P, 8);
@@ -502,7 +505,9 @@ int by_tile(const ProductArgs &a, hipStream_t st)
 {
     if constexpr (T::planes == 3) {
         // fp32: 128 x 256 or 128 x 128, one a CU; a round of the former has twice the work in 1.45 to 1.7 of the time (4040 tokens,
-        // 1024 x 2600: a and u in 3 rounds 285 us, 6 of small ones 336; dx, whose large tiles are half a round, 416 and 282)
+        // 1024 x 2600: a and u in 3 rounds 285 us, 6 of small ones 336; dx, whose large tiles are half a round, 416 and 282).  It does not look at the files' tokens:
+        // where they are few a tile has one step, and a training step takes longer than one of the library's fp32 products (20 files of 8
+        // tokens 663 us and 425, 64 of 8 1060 and 858; 20 of 64 815 and 932).
         const auto rounds = [&](uint32_t m) {
             return (double)cdiv((uint64_t)cdiv(a.rows_n, WHAT == Product::gated ? 64 : 128) * cdiv(a.rows_m, m) * a.files * a.halves, 256);
         };

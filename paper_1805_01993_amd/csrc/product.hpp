@@ -83,7 +83,8 @@ __device__ __forceinline__ void store_side(uint16_t *p, int64_t plane, const Eig
     }
 }
 
-// The activation of a and its derivative.
+// The activation of a and its derivative.  16-bit modes: the hardware's exponential of x, some |x| 2^-24 of its value off, which the
+// rounding of h to 8 or 11 bits hides (8192 rows of 4096 x 11264 bf16 1919 us, with expf 1945).
 template <class T>
 __device__ __forceinline__ void activate(int which, float a, float &value, float &slope)
 {
