@@ -5,7 +5,7 @@ its gradient.
   quantise  of each row, blocks of 128 columns: e the least whole number with max |x| <= 448 2^e (0 where the block is zero,
             at least -127), q = x 2^-e rounded to e4m3; rows are padded with zeros to whole blocks.  The scale is kept as e + 127,
             a row's blocks padded to a multiple of four with 127.
-  product8  y[m][n] = sum over blocks b of 2^(ex[m][b] + ew[n][b]) sum over the block's k of qx[m][k] qw[n][k]
+  product   y[m][n] = sum over blocks b of 2^(ex[m][b] + ew[n][b]) sum over the block's k of qx[m][k] qw[n][k]
   top       of each row, the k largest logits and their columns, larger ones first and of equal ones the lower column (-1 and
             -inf where a row has fewer above -inf), and rest = log of the sum of exp(z / T) over the columns not among them
   distill   p = softmax of (t_1 / T ... t_k / T, rest) (no last one where rest is not given), q = softmax(z / T),
@@ -33,7 +33,7 @@ def _quantise(rows, columns, mode, std=1.0):
 
 
 def _product(rows, inputs, outputs, mode):
-    return {"op": "product8", "rows": rows, "columns": inputs, "outputs": outputs, "mode": mode}
+    return {"op": "product", "rows": rows, "columns": inputs, "outputs": outputs, "mode": mode}
 
 
 def _top(rows, columns, k, mode, temperature=1.0, masked=0.0):
@@ -83,12 +83,12 @@ def draw(rng):
         return max(1, v // grain) * grain
 
     while True:
-        op = rng.choices(["quantise", "product8", "top", "distill"], [1, 3, 2, 3])[0]
+        op = rng.choices(["quantise", "product", "top", "distill"], [1, 3, 2, 3])[0]
         mode, grain = rng.choice(["bf16", "bf16", "f16", "f32"]), rng.choice([1, 1, 8, 64])
         temperature, masked = rng.choice([0.7, 1.0, 2.0]), rng.choice([0.0, 0.0, 0.03])
         if op == "quantise":
             case = _quantise(size(1, 65536), size(64, 16384, grain), mode, rng.choice([0.02, 1.0]))
-        elif op == "product8":
+        elif op == "product":
             rows = size(1, 64) if rng.random() < 0.4 else size(1, 8192, rng.choice([1, 16, 128]))
             case = _product(rows, size(128, 11264, grain), size(128, 32768, grain), mode)
         elif op == "top":
@@ -97,7 +97,7 @@ def draw(rng):
             case = _distill(rng.choice(["loss", "train", "train"]), size(1, 16384), size(100, 262144, grain), size(1, 128), mode,
                             temperature, rng.random() < 0.7, masked)
         values = case["rows"] * case["columns"]
-        most = {"quantise": 50021 * 2001, "product8": 1 << 40, "top": 4096 * 50021, "distill": 14336 * 32768}[op]
+        most = {"quantise": 50021 * 2001, "product": 1 << 40, "top": 4096 * 50021, "distill": 14336 * 32768}[op]
         need = work(case)
         if values <= most and need["flops"] <= 2 * 8192 * 4096 * 11264 and need["bytes"] <= 1.9e9:
             return case
@@ -113,7 +113,7 @@ def work(case):
     rows, columns, eb = case["rows"], case["columns"], BYTES[case["mode"]]
     if case["op"] == "quantise":
         return {"bytes": rows * (columns * eb + sum(_padded(columns))), "flops": 2 * rows * columns}
-    if case["op"] == "product8":
+    if case["op"] == "product":
         n = case["outputs"]
         return {"bytes": (rows + n) * sum(_padded(columns)) + rows * n * eb, "flops": 2 * rows * n * columns}
     if case["op"] == "top":
@@ -134,7 +134,7 @@ def _inputs(case, seed):
         # a few columns are much larger than the others, as activations have them
         loud = 1 + 30 * (torch.rand(columns, device="cuda", generator=g) < 0.01).float()
         return {"x": (normal(rows, columns, std=case["std"]) * loud).to(dtype)}
-    if case["op"] == "product8":
+    if case["op"] == "product":
         s = {}
         for name, n, std in (("x", rows, 1.0), ("w", case["outputs"], 1 / math.sqrt(columns))):
             s["q" + name], s["s" + name] = _plain_quantise(normal(n, columns, std=std))
@@ -175,7 +175,7 @@ def prepare(case, seed):
     if case["op"] == "quantise":
         wide, blocks = _padded(columns)
         s["q"], s["scale"] = new(torch.float8_e4m3fn, rows, wide), new(torch.uint8, rows, blocks)
-    elif case["op"] == "product8":
+    elif case["op"] == "product":
         s["y"] = new(dtype, rows, case["outputs"])
     elif case["op"] == "top":
         k = case["k"]
@@ -199,7 +199,7 @@ def run(state):
     if case["op"] == "quantise":
         q, scale = _plain_quantise(s["x"].float())
         return {"q": q, "scale": scale}
-    if case["op"] == "product8":
+    if case["op"] == "product":
         return {"y": (_wide(s["qx"], s["sx"]) @ _wide(s["qw"], s["sw"]).t()).to(TYPES[case["mode"]])}
     return _plain_top(s) if case["op"] == "top" else _plain_distill(s)
 
@@ -209,8 +209,8 @@ def _run_own(s):
     if case["op"] == "quantise":
         block.quantise(s["x"], s["q"], s["scale"])
         return {"q": s["q"], "scale": s["scale"]}
-    if case["op"] == "product8":
-        block.product8(s["qx"], s["sx"], s["qw"], s["sw"], s["y"])
+    if case["op"] == "product":
+        block.packed_product(s["qx"], s["sx"], s["qw"], s["sw"], s["y"])
         return {"y": s["y"]}
     if case["op"] == "top":
         block.top(s["z"], s["index"], s["value"], rest=s["rest"], temperature=case["temperature"])
@@ -309,7 +309,7 @@ def exact(case, seed):
     s = _inputs(case, seed)
     if case["op"] == "quantise":
         return _exact_quantise(s["x"].double())
-    if case["op"] == "product8":
+    if case["op"] == "product":
         values = []
         for name in ("x", "w"):
             power = torch.repeat_interleave(s["s" + name].long() - 127, BLOCK, 1)[:, :s["q" + name].shape[1]]
