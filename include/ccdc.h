@@ -412,6 +412,64 @@ int ccdc_dropout(const ccdc_block_t *block, int64_t rows, int64_t columns, doubl
                  const void *x, int64_t ldx, const void *residual, int64_t ld_residual, void *y, int64_t ldy,
                  void *stream);
 
+/*
+ * Learning from a teacher that answers in 8 bits: matrices held in 8-bit floating point, their product, the top logits of
+ * an answer, and what a student that answers otherwise loses, with its gradient.  A teacher's weights are quantised once; then
+ *
+ *   ccdc_quantise         x  ->  8-bit numbers with a scale for each block of 128 columns
+ *   ccdc_packed_product   y = x W'  of two such matrices
+ *   ccdc_top              of each row of y, its k largest logits, their columns, and what all others come to
+ *   ccdc_distill          of each row of a student's logits, its distance from the teacher's, and the gradient
+ *
+ * These calls use of the block its elements (the mode's) and its device, and nothing else of it: rows and columns are the
+ * call's own, no workspace is used, and calls on one block may run on several streams at once.  As the calls above they need an
+ * uploaded block on the current device, enqueue kernels on `stream` and allocate nothing.  Sums are carried in fp32 and have one
+ * order: a row's results depend on the row alone (a product's on both matrices' sizes too).
+ * CCDC_EINVAL for a null pointer (where NULL has no meaning given), one not aligned to its element, a size below 1 (0 rows are
+ * nothing to do) or a stride below the width; CCDC_ESIZE where a size, a launch or a row passes what the call takes.  Outputs
+ * are written in full and overlap no input unless that is said.
+ */
+
+/* A packed matrix, in 8 bits: rows of numbers of 8 bits (e4m3: one sign, four exponent and three mantissa bits, largest 448, no
+ * infinities), as many as `columns` rounded up to a multiple of 128, contiguous, aligned to 16 bytes, zeros past `columns`;
+ * and for each row as many bytes as it has blocks of 128, rounded up to a multiple of 4, contiguous, aligned to 4, of which byte b is
+ * e + 127 for the block of columns 128 b ..: the numbers stand for q 2^e.  Bytes past the last block are 127.  (254 is the largest
+ * scale; a block with a scale of 255 is no number.) */
+
+/* q and scale of x [rows][columns]: e is the least whole number, at least -127, with |x| <= 448 2^e for all finite numbers of the block,
+ * 0 where these are zeros; q = x 2^-e rounded to nearest even; an infinity or a NaN is a NaN there and changes nothing else. */
+int ccdc_quantise(const ccdc_block_t *block, int64_t rows, int64_t columns, const void *x, int64_t ldx, void *q, void *scale,
+                  void *stream);
+
+/* y [rows][outputs] = x W' of packed x [rows][columns] and W [outputs][columns].  CCDC_ESIZE for columns above 2^20 or more than
+ * 2^31 - 1 rows or outputs.  With 16-bit results the matrix instructions add eight products at a time, of which they drop what is below
+ * 2^-13 of the largest of the eight; with fp32 results they keep it. */
+int ccdc_packed_product(const ccdc_block_t *block, int64_t rows, int64_t outputs, int64_t columns, const void *x,
+                        const void *x_scale, const void *W, const void *W_scale, void *y, int64_t ldy, void *stream);
+
+/* The k largest of each row of z [rows][columns], 1 <= k <= 128: index [rows][k] their columns and value [rows][k] themselves, larger
+ * ones first and of equal ones the lower column.  What is -infinity (masked) or a NaN is not among them; where a row has fewer, index is
+ * -1 and value -infinity.  rest [rows] (NULL: not wanted): the logarithm of the sum of exp(z / temperature) over all other
+ * columns, -infinity where there are none; a NaN in the row makes it one.  CCDC_ESIZE for columns above 2^20. */
+int ccdc_top(const ccdc_block_t *block, int64_t rows, int64_t columns, const void *z, int64_t ldz, int k, double temperature,
+             int32_t *index, float *value, float *rest, void *stream);
+
+/* The distance of a student's logits z [rows][columns] from a teacher's answer, as ccdc_top gives it: index, value [rows][k],
+ * 1 <= k <= 128, and rest [rows] at the same temperature.  With T the temperature, p = softmax(value / T ..., rest) over the k listed
+ * columns and, together as one more, all others, q = softmax(z / T), and q_rest the sum of q over these others:
+ *
+ *   loss = weight scale (sum over the listed j of p_j log(p_j / q_j) + p_rest log(p_rest / q_rest))
+ *
+ * and dz is the gradient of it.  rest NULL (or -infinity): p_rest = 0, the teacher's answer is its list alone; with k = 1 that is the cross
+ * entropy of a label.  weight [rows] (NULL: ones): a row of weight 0 has zeros, whatever its logits.  An entry with an
+ * index outside 0 .. columns - 1, or that of an entry before it, is none; a row without entries, or whose values (and
+ * rest) or logits are all -infinity, has nothing to learn: zeros.  A term with p = 0 is 0.  A NaN or +infinity among the logits makes the row's results NaN.
+ * loss [rows] and dz [rows][columns] may be NULL: not wanted (not both).  dz may be z (then lddz = ldz).  CCDC_ESIZE for columns
+ * above 2^20. */
+int ccdc_distill(const ccdc_block_t *block, int64_t rows, int64_t columns, const void *z, int64_t ldz, int k, const int32_t *index,
+                 const float *value, const float *rest, double temperature, const float *weight, double scale, float *loss,
+                 void *dz, int64_t lddz, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,4 +15,5 @@ from .binding import (  # noqa: F401
     ccdc_plan_jobs,
     ccdc_plan_jobs_repeated,
     load_library,
+    packed_shapes,
 )

@@ -42,6 +42,7 @@ EXPORTS = [
     "ccdc_node_decode_reduce",
     "ccdc_block", "ccdc_block_destroy", "ccdc_block_bind", "ccdc_block_upload", "ccdc_block_query",
     "ccdc_ffn_forward", "ccdc_ffn_backward", "ccdc_join_forward", "ccdc_join_backward", "ccdc_dropout",
+    "ccdc_quantise", "ccdc_packed_product", "ccdc_top", "ccdc_distill",
 ]
 
 
@@ -57,8 +58,10 @@ _CALLS = [("ccdc_pipeline_fused", False, "V X Phi"), ("ccdc_pipeline_fused_noall
           ("ccdc_map", False, "V Phi V"), ("ccdc_combine", False, "V Vbar"), ("ccdc_encode", False, "Vbar X"),
           ("ccdc_decode", False, "X Vbar D"), ("ccdc_reduce", False, "V D Phi"), ("ccdc_shuffle_fused", False, "V X D"),
           ("ccdc_node_encode", True, "V X"), ("ccdc_node_decode_reduce", True, "V X Phi")]
-_BLOCK_CALLS = ("ccdc_ffn_forward", "ccdc_ffn_backward", "ccdc_join_forward", "ccdc_join_backward", "ccdc_dropout")
-_FFN_FORWARD, _FFN_BACKWARD, _JOIN_FORWARD, _JOIN_BACKWARD, _DROPOUT = range(len(_BLOCK_CALLS))
+_BLOCK_CALLS = ("ccdc_ffn_forward", "ccdc_ffn_backward", "ccdc_join_forward", "ccdc_join_backward", "ccdc_dropout",
+                "ccdc_quantise", "ccdc_packed_product", "ccdc_top", "ccdc_distill")
+(_FFN_FORWARD, _FFN_BACKWARD, _JOIN_FORWARD, _JOIN_BACKWARD, _DROPOUT, _QUANTISE, _PACKED_PRODUCT, _TOP,
+ _DISTILL) = range(len(_BLOCK_CALLS))
 (_PIPELINE, _PIPELINE_NOALLOC, _MAP, _COMBINE, _ENCODE, _DECODE, _REDUCE, _SHUFFLE, _NODE_ENCODE,
  _NODE_DECODE) = range(len(_CALLS))
 
@@ -124,7 +127,11 @@ def load_library():
                        ("ccdc_ffn_backward", [vp, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]),
                        ("ccdc_join_forward", [vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, i64, u64, vp]),
                        ("ccdc_join_backward", [vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, i64, vp, vp, vp, i64, u64, vp]),
-                       ("ccdc_dropout", [vp, i64, i64, C.c_double, C.c_uint32, u64, vp, i64, vp, i64, vp, i64, vp])):
+                       ("ccdc_dropout", [vp, i64, i64, C.c_double, C.c_uint32, u64, vp, i64, vp, i64, vp, i64, vp]),
+                       ("ccdc_quantise", [vp, i64, i64, vp, i64, vp, vp, vp]),
+                       ("ccdc_packed_product", [vp, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp]),
+                       ("ccdc_top", [vp, i64, i64, vp, i64, C.c_int, C.c_double, vp, vp, vp, vp]),
+                       ("ccdc_distill", [vp, i64, i64, vp, i64, C.c_int, vp, vp, vp, C.c_double, vp, C.c_double, vp, vp, i64, vp])):
         fn = getattr(lib, name)
         fn.restype = C.c_int
         fn.argtypes = args
@@ -621,6 +628,93 @@ class Block:
             self._h, rows, columns, p, site, seed, self._matrix(x, "x", columns), self._ld(x),
             self._matrix(residual, "residual", columns, rows), self._ld(residual), self._matrix(y, "y", columns, rows),
             self._ld(y), _stream_ptr(stream)), "ccdc_dropout")
+
+    # ---- learning from a teacher that answers in 8 bits
+    def _logits(self, t, name, columns=None, rows=None):
+        """Address and row stride of a matrix on the current device."""
+        if t is None:
+            return None, 0
+        self._here(t, name)
+        if t.dim() != 2:
+            raise ValueError(f"{name}: need a matrix, got {list(t.shape)}")
+        return self._matrix(t, name, t.shape[1] if columns is None else columns, rows), self._ld(t)
+
+    @staticmethod
+    def _here(t, name):
+        import torch
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name}: need a tensor on the current device, got one on {t.device}")
+
+    def _plain(self, t, name, dtypes, shape):
+        """Address of a contiguous tensor that is not of the block's elements (None: null)."""
+        if t is None:
+            return None
+        self._here(t, name)
+        if t.dtype not in dtypes or list(t.shape) != list(shape) or not t.is_contiguous():
+            raise ValueError(f"{name}: need {list(shape)} of {dtypes[0]}, contiguous, got {list(t.shape)} of {t.dtype}")
+        return t.data_ptr()
+
+    def _eight(self, q, scale, name, columns=None, rows=None):
+        """Addresses of a matrix in 8 bits and of its scales."""
+        import torch
+        if q.dim() != 2 or q.shape[1] == 0 or q.shape[1] % 128:
+            raise ValueError(f"{name}: need rows of whole blocks of 128, got {list(q.shape)}")
+        shapes = packed_shapes(q.shape[0] if rows is None else rows, q.shape[1] if columns is None else columns)
+        return (self._plain(q, name, (torch.float8_e4m3fn, torch.uint8), shapes[0]),
+                self._plain(scale, name + "'s scale", (torch.uint8,), shapes[1]))
+
+    def quantise(self, x, q, scale, stream=None):
+        """x as numbers of 8 bits (torch.float8_e4m3fn, or uint8 for their bits) with a scale for each block of 128; packed_shapes
+        has the shapes of q and scale (uint8)."""
+        if stream is None and self._quick(_QUANTISE, x, q, scale) == OK:
+            return
+        px, ld = self._logits(x, "x")
+        pq, ps = self._eight(q, scale, "q", x.shape[1], x.shape[0])
+        _check(self._lib.ccdc_quantise(self._h, x.shape[0], x.shape[1], px, ld, pq, ps, _stream_ptr(stream)), "ccdc_quantise")
+
+    def packed_product(self, x, x_scale, W, W_scale, y, stream=None):
+        """y [rows][outputs] = x W' of x [rows] and W [outputs], both in 8 bits and of as many columns."""
+        if stream is None and self._quick(_PACKED_PRODUCT, x, x_scale, W, W_scale, y) == OK:
+            return
+        px, psx = self._eight(x, x_scale, "x")
+        pw, psw = self._eight(W, W_scale, "W", x.shape[1])
+        py, ld = self._logits(y, "y", W.shape[0], x.shape[0])
+        _check(self._lib.ccdc_packed_product(self._h, x.shape[0], W.shape[0], x.shape[1], px, psx, pw, psw, py, ld, _stream_ptr(stream)),
+               "ccdc_packed_product")
+
+    def top(self, z, index, value, rest=None, temperature=1.0, stream=None):
+        """The k largest logits of every row: index (int32) and value (float32) [rows][k], and rest [rows], the logarithm of the sum
+        of exp(z / temperature) over all others."""
+        if stream is None and self._quick(_TOP, z, index, value, rest, temperature) == OK:
+            return
+        import torch
+        pz, ld = self._logits(z, "z")
+        rows, k = z.shape[0], index.shape[-1]
+        _check(self._lib.ccdc_top(
+            self._h, rows, z.shape[1], pz, ld, k, temperature, self._plain(index, "index", (torch.int32,), (rows, k)),
+            self._plain(value, "value", (torch.float32,), (rows, k)), self._plain(rest, "rest", (torch.float32,), (rows,)),
+            _stream_ptr(stream)), "ccdc_top")
+
+    def distill(self, z, index, value, loss, dz, rest=None, temperature=1.0, weight=None, scale=1.0, stream=None):
+        """Of a student's logits z against what top gave of a teacher's: loss [rows] (float32) and its gradient dz; either None: not
+        wanted; dz may be z.  weight [rows] (float32): 0 for rows that count for nothing."""
+        if stream is None and self._quick(_DISTILL, z, index, value, loss, dz, rest, temperature, weight, scale) == OK:
+            return
+        import torch
+        pz, ldz = self._logits(z, "z")
+        rows, k = z.shape[0], index.shape[-1]
+        pdz, lddz = self._logits(dz, "dz", z.shape[1], rows)
+        of_rows = [self._plain(t, name, (torch.float32,), (rows,)) for t, name in ((rest, "rest"), (weight, "weight"), (loss, "loss"))]
+        _check(self._lib.ccdc_distill(
+            self._h, rows, z.shape[1], pz, ldz, k, self._plain(index, "index", (torch.int32,), (rows, k)),
+            self._plain(value, "value", (torch.float32,), (rows, k)), of_rows[0], temperature, of_rows[1], scale, of_rows[2], pdz, lddz,
+            _stream_ptr(stream)), "ccdc_distill")
+
+
+def packed_shapes(rows, columns):
+    """Shapes of a [rows][columns] matrix in 8 bits: of its numbers, and of its scales."""
+    blocks = -(-columns // 128)
+    return (rows, blocks * 128), (rows, -(-blocks // 4) * 4)
 
 
 def ccdc_block(width, hidden, mode, **config):

@@ -1,0 +1,225 @@
+// The distance of a student's logits from a teacher's top logits, and its gradient: one pass over the row.
+//
+// With S the listed columns and e_v = exp((z_v - m) / T), m the largest logit outside S and s the sum of e_v there, all that a row of others
+// needs is one number: dz_v = w C e_v with C = exp(m / T - lse) - p_rest / s, lse over the whole row.  So the others' sums are
+// their own (a difference of the whole row's and the list's would lose them where the list has nearly everything), and the
+// list's k columns are one wavefront's, two a lane.  A bit a column in LDS says which are listed.
+//
+// The row is held in registers as loaded between the sums and the gradient: read once, written once.
+#include "vocabulary.hpp"
+
+namespace {
+using namespace ccdc;
+
+struct DistillArgs {
+    const void *z;
+    const int32_t *index;
+    const float *value, *rest, *weight;
+    float *loss;
+    void *dz;
+    int64_t ldz, lddz;
+    int32_t columns, k, mask_bytes;
+    float per_T, scale;                           // 1 / T
+};
+
+constexpr float kLog2e = 1.44269504f;
+
+// What the list's wavefront tells the others.
+struct Listed {
+    float most, sum;                              // of the listed logits: the largest, sum of exp((z - most) / T)
+    float p_rest;
+    int count;                                    // entries; 0 too where they and the rest are all -infinity
+};
+
+// Three terms' worth of rounding is all that exp(x) = 2^(x log2 e) adds in fp32 for what exp gives of |x| < 100.
+__device__ __forceinline__ float exponential(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+template <class T, int WAVES, int PACKS>
+__global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
+{
+    using E = typename T::elem;
+    constexpr int THREADS = 64 * WAVES;
+    extern __shared__ uint32_t mask[];            // a bit a column, lowest first
+    __shared__ float part[2 * WAVES];
+    __shared__ int32_t listed[kMostListed];
+    __shared__ Listed shared;
+    OverRow<WAVES> over{part};
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x % 64;
+    const bool lists = threadIdx.x < 64;          // the list's wavefront
+    const float factor = a.weight ? a.weight[row] * a.scale : a.scale;
+    const bool counts = !(a.weight && a.weight[row] == 0.0f);
+    Row<T, WAVES, PACKS> z;
+    if (counts) z.load(a.z, row * a.ldz, a.columns);
+    for (int i = threadIdx.x; i < a.mask_bytes / 4; i += THREADS) mask[i] = 0;
+
+    int32_t column[2] = {-1, -1};
+    float p[2] = {}, log_p[2] = {}, logit[2] = {-INFINITY, -INFINITY};
+    if (lists) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const int j = lane + 64 * h;
+            if (j < a.k) column[h] = a.index[row * a.k + j];
+            if ((uint32_t)column[h] >= (uint32_t)a.columns) column[h] = -1;
+            listed[j] = column[h];
+        }
+    }
+    __syncthreads();
+    if (lists) {
+        // an entry whose column was listed before is none
+        for (int i = 0; i < a.k; i++) {
+            const int32_t other = listed[i];
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+                if (i < lane + 64 * h && other == column[h]) column[h] = -1;
+        }
+        float t[2] = {-INFINITY, -INFINITY}, most = -INFINITY, count = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+            if (column[h] >= 0) {
+                t[h] = a.value[row * a.k + lane + 64 * h] * a.per_T;
+                logit[h] = T::widen(((const E *)a.z)[row * a.ldz + column[h]]);
+                atomicOr(&mask[column[h] / 32], 1u << (column[h] % 32));
+                count += 1.0f;
+                most = fmaxf(most, logit[h]);
+            }
+        // the teacher's p over the list and the rest
+        const float rest = a.rest ? a.rest[row] : -INFINITY;
+        const float top = fmaxf(fmaxf(wave_most(fmaxf(t[0], t[1])), rest), kLowest);
+        float sum = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2; h++) sum += exponential(t[h] - top);
+        const float of_rest = exponential(rest - top), total = wave_sum(sum) + of_rest, log_total = logf(total);
+#pragma unroll
+        for (int h = 0; h < 2; h++) p[h] = exponential(t[h] - top) / total, log_p[h] = t[h] - top - log_total;
+        most = wave_most(most);
+        float own = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+            if (column[h] >= 0) own += exponential((logit[h] - fmaxf(most, kLowest)) * a.per_T);
+        own = wave_sum(own);
+        count = wave_sum(count);
+        if (lane == 0) shared = {most, own, of_rest / total, total == 0.0f ? 0 : (int)count};
+    }
+    __syncthreads();
+    const Listed list = shared;
+    if (!counts || list.count == 0) {             // (the same for all threads)
+        if (a.loss && threadIdx.x == 0) a.loss[row] = 0.0f;
+        if (a.dz)
+            for (int32_t c = (int32_t)threadIdx.x * 8; c < a.columns; c += THREADS * 8) store_eight<T>((E *)a.dz + row * a.lddz + c, Eight{}, a.columns - c);
+        return;
+    }
+
+    const auto listed_of = [&](int32_t c) { return (mask[c / 32] >> (c % 32)) & 0xFFu; };
+    const float scale = a.per_T * kLog2e;
+    float m = -INFINITY, s = 0.0f;
+    if constexpr (PACKS > 0) {
+        z.hide_held(listed_of);
+        z.each(listed_of, [&](const Eight &v, int32_t, int32_t) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) m = fmaxf(m, v.v[i]);
+        });
+        m = over.most(m);
+        const float from = fmaxf(m, kLowest);
+        z.each(listed_of, [&](const Eight &v, int32_t, int32_t) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) s += __builtin_amdgcn_exp2f((v.v[i] - from) * scale);
+        });
+        s = over.sum(s);
+    } else {
+        // the largest so far and the sum from it on
+        z.each(listed_of, [&](const Eight &v, int32_t, int32_t) {
+            float next = m;
+#pragma unroll
+            for (int i = 0; i < 8; i++) next = fmaxf(next, v.v[i]);
+            const float from = fmaxf(next, kLowest);
+            s *= __builtin_amdgcn_exp2f((m - from) * scale);
+#pragma unroll
+            for (int i = 0; i < 8; i++) s += __builtin_amdgcn_exp2f((v.v[i] - from) * scale);
+            m = next;
+        });
+        const float own = m;
+        m = over.most(m);
+        s = over.sum(s * __builtin_amdgcn_exp2f((own - fmaxf(m, kLowest)) * scale));
+    }
+
+    // all relative to the row's largest logit
+    const float from = fmaxf(m, kLowest), top = fmaxf(fmaxf(m, list.most), kLowest);
+    const float others = (from - top) * a.per_T, others_exp = m > -INFINITY ? exponential(others) : 0.0f;
+    const float listed_exp = list.most > -INFINITY ? exponential((list.most - top) * a.per_T) : 0.0f;
+    const float total = s * others_exp + list.sum * listed_exp, lse = logf(total);
+    if (total == 0.0f) {                          // no logit above -infinity: nothing to learn
+        if (a.loss && threadIdx.x == 0) a.loss[row] = 0.0f;
+        if (a.dz)
+            for (int32_t c = (int32_t)threadIdx.x * 8; c < a.columns; c += THREADS * 8) store_eight<T>((E *)a.dz + row * a.lddz + c, Eight{}, a.columns - c);
+        return;
+    }
+    float gradient[2];
+    if (lists) {
+        float loss = 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const float log_q = (logit[h] - top) * a.per_T - lse;
+            if (column[h] >= 0 && !(p[h] == 0.0f)) loss += p[h] * (log_p[h] - log_q);
+            gradient[h] = factor * a.per_T * (exponential(log_q) - p[h]);
+        }
+        loss = wave_sum(loss);
+        if (lane == 0 && a.loss) {
+            if (!(list.p_rest == 0.0f)) loss += list.p_rest * (logf(list.p_rest) - (others + logf(s) - lse));
+            a.loss[row] = factor * loss;
+        }
+    }
+    if (!a.dz) return;
+    const float of_rest = list.p_rest == 0.0f || s == 0.0f ? 0.0f : list.p_rest / s;
+    const float C = factor * a.per_T * (others_exp / total - of_rest);
+    E *dz = (E *)a.dz + row * a.lddz;
+    z.each(listed_of, [&](const Eight &v, int32_t c, int32_t left) {
+        if (left <= 0) return;
+        Eight d;
+#pragma unroll
+        for (int i = 0; i < 8; i++) d.v[i] = C * __builtin_amdgcn_exp2f((v.v[i] - from) * scale);
+        store_eight<T>(dz + c, d, left);
+    });
+    __syncthreads();                              // the list's columns are written over
+    if (lists)
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+            if (column[h] >= 0) dz[column[h]] = narrow<T>(gradient[h]);
+}
+
+template <class T>
+int run_distill(const DistillArgs &a, int64_t rows, hipStream_t st)
+{
+    return by_columns<T>(a.columns, [&](auto waves, auto packs) -> int {
+        constexpr int W = decltype(waves)::value, P = decltype(packs)::value;
+        if (!fits_launch((uint64_t)rows * 64 * W)) return CCDC_ESIZE;
+        k_distill<T, W, P><<<(uint32_t)rows, 64 * W, a.mask_bytes, st>>>(a);
+        return launched();
+    });
+}
+
+}  // namespace
+
+extern "C" {
+
+int ccdc_distill(const ccdc_block_t *b, int64_t rows, int64_t columns, const void *z, int64_t ldz, int k, const int32_t *index,
+                 const float *value, const float *rest, double temperature, const float *weight, double scale, float *loss, void *dz,
+                 int64_t lddz, void *stream)
+{
+    const int rc = ready(b);
+    if (rc != CCDC_OK) return rc;
+    if (rows < 0 || columns < 1 || ldz < columns || k < 1 || k > kMostListed || (dz && lddz < columns)) return CCDC_EINVAL;
+    const float heat = (float)temperature, per_T = 1.0f / heat;
+    if (!(heat > 0.0f) || !std::isfinite(heat) || !std::isfinite(per_T) || !std::isfinite((float)scale)) return CCDC_EINVAL;
+    if (rows == 0) return CCDC_OK;
+    if (!loss && !dz) return CCDC_EINVAL;
+    if (!fits(b, z) || !fits(b, dz, true) || !index || !value || (dz && dz == z && lddz != ldz)) return CCDC_EINVAL;
+    for (const void *p : {(const void *)index, (const void *)value, (const void *)rest, (const void *)weight, (const void *)loss})
+        if (!aligned(p, 4)) return CCDC_EINVAL;
+    if (columns > kMostColumns) return CCDC_ESIZE;
+    const DistillArgs a{z, index, value, rest, weight, loss, dz, ldz, lddz, (int32_t)columns, k, (int32_t)((columns + 31) / 32 * 4), per_T,
+                        (float)scale};
+    CCDC_BY_ELEM(b, (run_distill<T>(a, rows, (hipStream_t)stream)));
+}
+
+}  // extern "C"

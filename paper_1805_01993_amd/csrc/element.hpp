@@ -1,6 +1,8 @@
 // What the kernels of a block share: element types, eight elements of a row at a time, dropout.
 #pragma once
 
+#include <type_traits>
+
 #include "block.hpp"
 #include "common.hpp"
 
@@ -186,6 +188,23 @@ __device__ __forceinline__ Eight dropout_factors(const Dropout &d, uint32_t id, 
 
 // What is taken out counts for nothing, whatever it was (an infinity or no number too).
 __device__ __forceinline__ float kept(float v, float factor) { return factor != 0.0f ? v * factor : 0.0f; }
+
+// The sum over a wavefront, the same for all its lanes: in sixteens by shifts within them, then from each sixteen to the next, in
+// registers (by exchanges through LDS 8 rows of 2048 bf16 values took 6.0 us, this way 5.6; large inputs 1 %).
+__device__ __forceinline__ float wave_sum(float v)
+{
+    const auto moved = [](float x, auto control, auto rows) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(control)::value, decltype(rows)::value, 15, true));
+    };
+    using std::integral_constant;
+    v += moved(v, integral_constant<int, 0x111>(), integral_constant<int, 15>());      // shifted by 1, 2, 4 and 8 lanes
+    v += moved(v, integral_constant<int, 0x112>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x114>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x118>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x142>(), integral_constant<int, 10>());      // lane 15 to the second sixteen, 47 to the fourth
+    v += moved(v, integral_constant<int, 0x143>(), integral_constant<int, 12>());      // lane 31 to the upper half
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
 
 inline int ready(const ccdc_block_t *b)
 {

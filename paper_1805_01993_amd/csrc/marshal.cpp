@@ -156,7 +156,7 @@ void marshal_dealloc(PyObject *self)
 
 // The calls of one bound block (ccdc_block), in the same manner: what binding.py's Block would hand over, or None.  A call of
 // ccdc_join_forward on eight rows took 10.7 us through Python, 6 of them the kernel.
-enum BlockCall { kFfnForward, kFfnBackward, kJoinForward, kJoinBackward, kDropout, kBlockCalls };
+enum BlockCall { kFfnForward, kFfnBackward, kJoinForward, kJoinBackward, kDropout, kQuantise, kPackedProduct, kTop, kDistill, kBlockCalls };
 
 struct BlockMarshal {
     PyObject_HEAD
@@ -237,6 +237,50 @@ struct Reader {
         int64_t files = m.files;
         return matrix(o, &files, m.width, ld);
     }
+    // For the calls that learn from a teacher.  A tensor of this type on the current device, contiguous, of these sizes (columns 0: a
+    // vector); None: null, where that may be.
+    void *plain(PyObject *o, at::ScalarType type, int64_t rows, int64_t columns, bool none = false)
+    {
+        if (none && o == Py_None) return nullptr;
+        const at::Tensor *t = tensor(o, false);
+        if (!t || t->scalar_type() != type || !here(*t) || !t->is_contiguous() || t->dim() != (columns ? 2 : 1) || t->size(0) != rows ||
+            (columns && t->size(1) != columns))
+            return (void *)fail();
+        return t->data_ptr();
+    }
+    // A matrix in 8 bits and its scales (rows, wide -1: any, then they are its own).
+    void *eight(PyObject *o, PyObject *scales, int64_t *rows, int64_t *wide, void **scale)
+    {
+        const at::Tensor *t = tensor(o, false);
+        if (!t || (t->scalar_type() != at::kFloat8_e4m3fn && t->scalar_type() != at::kByte) || t->dim() != 2) return (void *)fail();
+        if (*rows < 0) *rows = t->size(0);
+        if (*wide < 0) *wide = t->size(1);
+        if (*wide <= 0 || *wide % 128 != 0) return (void *)fail();
+        void *at = plain(o, t->scalar_type(), *rows, *wide);
+        *scale = plain(scales, at::kByte, *rows, (*wide / 128 + 3) / 4 * 4);
+        return at;
+    }
+    // A matrix of the block's elements, on the current device.
+    void *logits(PyObject *o, int64_t *rows, int64_t *columns, int64_t *ld, bool none = false)
+    {
+        if (none && o == Py_None) return nullptr;
+        const at::Tensor *t = tensor(o);
+        if (!t || t->dim() != 2 || !here(*t)) return (void *)fail();
+        if (*columns < 0) *columns = t->size(1);
+        return matrix(o, rows, *columns, ld);
+    }
+    bool here(const at::Tensor &t) { return t.get_device() == c10::hip::current_device(); }
+    double real(PyObject *o)
+    {
+        if (!PyFloat_CheckExact(o)) ok = false;
+        return ok ? PyFloat_AS_DOUBLE(o) : 0.0;
+    }
+    int64_t listed(PyObject *o)               // columns of a list
+    {
+        const at::Tensor *t = tensor(o, false);
+        if (!t || t->dim() != 2 || t->size(1) < 1) fail();
+        return ok ? t->size(1) : 0;
+    }
     unsigned long long number(PyObject *o)
     {
         if (!ok || !PyLong_CheckExact(o)) {
@@ -268,13 +312,17 @@ using FfnForward = int (*)(const void *, int64_t, p, int64_t, p, p, p, int64_t, 
 using FfnBackward = int (*)(const void *, p, int64_t, p, p, p, p, int64_t, p, int64_t, p, int64_t, p, int64_t, p);
 using JoinForward = int (*)(const void *, int64_t, p, p, p, p, int64_t, p, p, p, int64_t, uint64_t, p);
 using JoinBackward = int (*)(const void *, p, p, p, p, p, p, int64_t, p, p, p, int64_t, p, p, p, int64_t, uint64_t, p);
+using Quantise = int (*)(const void *, int64_t, int64_t, p, int64_t, p, p, p);
+using PackedProduct = int (*)(const void *, int64_t, int64_t, int64_t, p, p, p, p, p, int64_t, p);
+using Top = int (*)(const void *, int64_t, int64_t, p, int64_t, int, double, p, p, p, p);
+using Distill = int (*)(const void *, int64_t, int64_t, p, int64_t, int, p, p, p, double, p, double, p, p, int64_t, p);
 using DropoutCall = int (*)(const void *, int64_t, int64_t, double, uint32_t, uint64_t, p, int64_t, p, int64_t, p, int64_t, p);
 
 // block(call, argument, ...) in the order of binding.py's methods
 PyObject *block_call(PyObject *self, PyObject *const *args, size_t nargsf, PyObject *kwnames)
 {
     const BlockMarshal &m = *reinterpret_cast<const BlockMarshal *>(self);
-    static constexpr Py_ssize_t count[kBlockCalls] = {6, 8, 8, 13, 6};
+    static constexpr Py_ssize_t count[kBlockCalls] = {6, 8, 8, 13, 6, 3, 5, 5, 9};
     const Py_ssize_t n = PyVectorcall_NARGS(nargsf);
     if (kwnames || n < 1 || at::impl::torch_function_mode_enabled()) Py_RETURN_NONE;
     const long id = PyLong_AsLong(args[0]);
@@ -339,6 +387,57 @@ PyObject *block_call(PyObject *self, PyObject *const *args, size_t nargsf, PyObj
             Py_END_ALLOW_THREADS
             break;
         }
+        case kQuantise: {
+            int64_t columns = -1;
+            p x = r.logits(a[0], &rows, &columns, &l[0]);
+            if (!r.ok || columns < 1) Py_RETURN_NONE;
+            int64_t wide = (columns + 127) / 128 * 128;
+            p scale, q = r.eight(a[1], a[2], &rows, &wide, &scale);
+            if (!r.ok) Py_RETURN_NONE;
+            Py_BEGIN_ALLOW_THREADS
+            status = reinterpret_cast<Quantise>(m.fn[id])(m.block, rows, columns, x, l[0], q, scale, stream);
+            Py_END_ALLOW_THREADS
+            break;
+        }
+        case kPackedProduct: {
+            int64_t wide = -1, outputs = -1;
+            p x_scale, w_scale, x = r.eight(a[0], a[1], &rows, &wide, &x_scale), w = r.eight(a[2], a[3], &outputs, &wide, &w_scale);
+            p y = r.ok ? r.logits(a[4], &rows, &outputs, &l[0]) : nullptr;
+            if (!r.ok) Py_RETURN_NONE;
+            Py_BEGIN_ALLOW_THREADS
+            status = reinterpret_cast<PackedProduct>(m.fn[id])(m.block, rows, outputs, wide, x, x_scale, w, w_scale, y, l[0], stream);
+            Py_END_ALLOW_THREADS
+            break;
+        }
+        case kTop: {
+            int64_t columns = -1;
+            p z = r.logits(a[0], &rows, &columns, &l[0]);
+            const int64_t k = r.listed(a[1]);
+            p index = r.plain(a[1], at::kInt, rows, k), value = r.plain(a[2], at::kFloat, rows, k), rest = r.plain(a[3], at::kFloat, rows, 0, true);
+            const double temperature = r.real(a[4]);
+            if (!r.ok || k > INT32_MAX) Py_RETURN_NONE;
+            Py_BEGIN_ALLOW_THREADS
+            status = reinterpret_cast<Top>(m.fn[id])(m.block, rows, columns, z, l[0], (int)k, temperature, index, value, rest, stream);
+            Py_END_ALLOW_THREADS
+            break;
+        }
+        case kDistill: {
+            int64_t columns = -1;
+            p z = r.logits(a[0], &rows, &columns, &l[0]);
+            const int64_t k = r.listed(a[1]);
+            p index = r.plain(a[1], at::kInt, rows, k), value = r.plain(a[2], at::kFloat, rows, k), loss = r.plain(a[3], at::kFloat, rows, 0, true);
+            p dz = r.ok ? r.logits(a[4], &rows, &columns, &l[1], true) : nullptr, rest = r.plain(a[5], at::kFloat, rows, 0, true);
+            const double temperature = r.real(a[6]);
+            p weight = r.plain(a[7], at::kFloat, rows, 0, true);
+            const double scale = r.real(a[8]);
+            if (!r.ok || k > INT32_MAX) Py_RETURN_NONE;
+            if (dz == nullptr) l[1] = 0;
+            Py_BEGIN_ALLOW_THREADS
+            status = reinterpret_cast<Distill>(m.fn[id])(m.block, rows, columns, z, l[0], (int)k, index, value, rest, temperature, weight, scale,
+                                                         loss, dz, l[1], stream);
+            Py_END_ALLOW_THREADS
+            break;
+        }
         default: {
             const at::Tensor *t = r.tensor(a[0]);
             if (!t || t->dim() != 2 || !PyFloat_CheckExact(a[2])) Py_RETURN_NONE;
@@ -366,8 +465,8 @@ PyObject *block_new(PyTypeObject *type, PyObject *args, PyObject *)
     unsigned long long block, fn[kBlockCalls];
     long long format, width, hidden, tokens, files, saved;
     PyObject *fail;
-    if (!PyArg_ParseTuple(args, "KOLLLLLLKKKKK", &block, &fail, &format, &width, &hidden, &tokens, &files, &saved, &fn[0], &fn[1], &fn[2],
-                          &fn[3], &fn[4]))
+    if (!PyArg_ParseTuple(args, "KOLLLLLLKKKKKKKKK", &block, &fail, &format, &width, &hidden, &tokens, &files, &saved, &fn[0], &fn[1], &fn[2],
+                          &fn[3], &fn[4], &fn[5], &fn[6], &fn[7], &fn[8]))
         return nullptr;
     PyObject *self = type->tp_alloc(type, 0);
     if (!self) return nullptr;

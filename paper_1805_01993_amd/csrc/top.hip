@@ -1,0 +1,201 @@
+// The largest logits of rows, in order, and the logarithm of what all others come to.
+//
+// A workgroup has a row, held in registers where it fits.  The k-th largest of the threads' own largest values is a bound that at
+// least k values reach and few more: with each thread's value in LDS, sixteen bounds at a time are counted by ballots, so five rounds find
+// twenty bits of it.  What reaches it is put into a list in LDS, whatever the order, and ranked there: as keys of 64 bits, value then
+// column, no two are equal, so the order is one.  A row of which too much reaches the bound (many equal values) is counted again
+// bit by bit, values first and then columns, until exactly k are left.
+#include "vocabulary.hpp"
+
+namespace {
+using namespace ccdc;
+
+struct TopArgs {
+    const void *z;
+    int32_t *index;
+    float *value, *rest;
+    int64_t ldz;
+    int32_t columns, k;
+    float per_T;
+};
+
+constexpr float kLog2e = 1.44269504f;
+
+// A number that grows with v, and 0 for what is never listed: -infinity and NaNs.
+__device__ __forceinline__ uint32_t ordered(float v)
+{
+    const uint32_t u = __float_as_uint(v + 0.0f);             // (no negative zero)
+    return v > -INFINITY ? u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u) : 0u;
+}
+__device__ __forceinline__ float value_of(uint32_t key)
+{
+    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
+template <class T, int WAVES, int PACKS>
+__global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
+{
+    constexpr int THREADS = 64 * WAVES, DIGITS = 16 / WAVES, ROUNDS = std::is_same<T, ElemBF16>::value ? 4 : 5;
+    constexpr int kRoom = WAVES <= 2 ? THREADS * PACKS * 8 : 2048;      // of the list
+    __shared__ float part[2 * WAVES];
+    __shared__ uint32_t largest[THREADS];
+    __shared__ int32_t counts[2][16];
+    __shared__ uint64_t found[kRoom];
+    __shared__ int32_t used;
+    __shared__ uint64_t last;
+    OverRow<WAVES> over{part};
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const auto none = [](int32_t) { return 0u; };
+    Row<T, WAVES, PACKS> z;
+    z.load(a.z, row * a.ldz, a.columns);
+    z.hide_held(none);
+
+    float most = -INFINITY;
+    z.each(none, [&](const Eight &v, int32_t, int32_t) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) most = fmaxf(most, v.v[i]);
+    });
+    const uint32_t own = ordered(most);
+    largest[threadIdx.x] = own;
+    if (threadIdx.x == 0) used = 0, last = 0;
+    __syncthreads();
+    uint32_t all[WAVES], bound = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; i++) all[i] = largest[i * 64 + lane];
+#pragma unroll
+    for (int round = 0; round < ROUNDS; round++) {
+        const int shift = 28 - 4 * round;
+#pragma unroll
+        for (int d = 0; d < DIGITS; d++) {
+            const int digit = wave * DIGITS + d;
+            const uint32_t from = bound | (uint32_t)digit << shift;
+            int count = 0;
+#pragma unroll
+            for (int i = 0; i < WAVES; i++) count += __popcll(__ballot(all[i] >= from));
+            if (lane == 0) counts[round % 2][digit] = count;
+        }
+        __syncthreads();
+        const uint32_t reach = (uint32_t)__ballot(lane < 16 && counts[round % 2][lane % 16] >= a.k) | 1u;
+        bound |= (uint32_t)(31 - __builtin_clz(reach)) << shift;
+    }
+    bound = max(bound, 1u);
+
+    const auto collect = [&](auto wanted) {
+        z.each(none, [&](const Eight &v, int32_t c, int32_t) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t key = ordered(v.v[i]);
+                if (wanted(key, c + i)) {
+                    const int at = atomicAdd(&used, 1);
+                    if (at < kRoom) found[at] = (uint64_t)key << 32 | (0xFFFFFFFFu - (uint32_t)(c + i));
+                }
+            }
+        });
+    };
+    if (own >= bound) collect([&](uint32_t key, int32_t) { return key >= bound; });
+    __syncthreads();
+    int32_t n = used;
+    if (n > kRoom) {                              // (the same for all threads)
+        const auto count = [&](auto wanted) {
+            float sum = 0.0f;
+            z.each(none, [&](const Eight &v, int32_t c, int32_t) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) sum += wanted(ordered(v.v[i]), c + i) ? 1.0f : 0.0f;
+            });
+            return (int32_t)over.sum(sum);        // (whole numbers below 2^24)
+        };
+        uint32_t key = 0, column = 0;             // of the k-th
+        for (int bit = 31; bit >= 0; bit--) {
+            const uint32_t next = key | 1u << bit;
+            if (count([&](uint32_t v, int32_t) { return v >= next; }) >= a.k) key = next;
+        }
+        const int32_t equal = a.k - count([&](uint32_t v, int32_t) { return v > key; });
+        for (int bit = 19; bit >= 0; bit--) {
+            const uint32_t next = column | 1u << bit;
+            if (count([&](uint32_t v, int32_t c) { return v == key && (uint32_t)c < next; }) < equal) column = next;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) used = 0;
+        __syncthreads();
+        collect([&](uint32_t v, int32_t c) { return v > key || (v == key && (uint32_t)c <= column); });
+        __syncthreads();
+        n = used;
+    }
+
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        const uint64_t mine = found[i];
+        int rank = 0;
+        for (int j = 0; j < n; j++) rank += found[j] > mine ? 1 : 0;
+        if (rank >= a.k) continue;
+        a.index[row * a.k + rank] = (int32_t)(0xFFFFFFFFu - (uint32_t)mine);
+        a.value[row * a.k + rank] = value_of((uint32_t)(mine >> 32));
+        if (rank == a.k - 1) last = mine;
+    }
+    for (int i = n + threadIdx.x; i < a.k; i += THREADS) {
+        a.index[row * a.k + i] = -1;
+        a.value[row * a.k + i] = -INFINITY;
+    }
+    if (!a.rest) return;
+    __syncthreads();
+    // What is not listed is at most the last that is: that is what it is summed from, and where so little is left of it that fp32 would
+    // lose it, its own largest.
+    const uint64_t kth = last;
+    const float least = kth ? value_of((uint32_t)(kth >> 32)) : -INFINITY, scale = a.per_T * kLog2e;
+    const int32_t column = kth ? (int32_t)(0xFFFFFFFFu - (uint32_t)kth) : -1;
+    const auto not_listed = [&](float v, int32_t c) { return v > least || (v == least && c <= column) ? -INFINITY : v; };
+    float from = fmaxf(least, kLowest);
+    const auto sum_from = [&] {
+        float sum = 0.0f;
+        z.each(none, [&](const Eight &v, int32_t c, int32_t) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) sum += __builtin_amdgcn_exp2f((not_listed(v.v[i], c + i) - from) * scale);
+        });
+        return over.sum(sum);
+    };
+    float sum = sum_from();
+    if (sum < 1e-30f) {                           // (the same for all threads)
+        float own_most = -INFINITY;
+        z.each(none, [&](const Eight &v, int32_t c, int32_t) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) own_most = fmaxf(own_most, not_listed(v.v[i], c + i));
+        });
+        from = fmaxf(over.most(own_most), kLowest);
+        sum = sum_from();
+    }
+    if (threadIdx.x == 0) a.rest[row] = from * a.per_T + logf(sum);
+}
+
+template <class T>
+int run_top(const TopArgs &a, int64_t rows, hipStream_t st)
+{
+    return by_columns<T>(a.columns, [&](auto waves, auto packs) -> int {
+        constexpr int W = decltype(waves)::value, P = decltype(packs)::value;
+        if (!fits_launch((uint64_t)rows * 64 * W)) return CCDC_ESIZE;
+        k_top<T, W, P><<<(uint32_t)rows, 64 * W, 0, st>>>(a);
+        return launched();
+    });
+}
+
+}  // namespace
+
+extern "C" {
+
+int ccdc_top(const ccdc_block_t *b, int64_t rows, int64_t columns, const void *z, int64_t ldz, int k, double temperature, int32_t *index,
+             float *value, float *rest, void *stream)
+{
+    const int rc = ready(b);
+    if (rc != CCDC_OK) return rc;
+    if (rows < 0 || columns < 1 || ldz < columns || k < 1 || k > kMostListed) return CCDC_EINVAL;
+    const float heat = (float)temperature, per_T = 1.0f / heat;
+    if (!(heat > 0.0f) || !std::isfinite(heat) || !std::isfinite(per_T)) return CCDC_EINVAL;
+    if (rows == 0) return CCDC_OK;
+    if (!fits(b, z) || !index || !value) return CCDC_EINVAL;
+    for (const void *p : {(const void *)index, (const void *)value, (const void *)rest})
+        if (!aligned(p, 4)) return CCDC_EINVAL;
+    if (columns > kMostColumns) return CCDC_ESIZE;
+    const TopArgs a{z, index, value, rest, ldz, (int32_t)columns, k, per_T};
+    CCDC_BY_ELEM(b, (run_top<T>(a, rows, (hipStream_t)stream)));
+}
+
+}  // extern "C"
