@@ -39,8 +39,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
 {
     using E = typename T::elem;
     constexpr int THREADS = 64 * WAVES;
+    constexpr bool kept = PACKS > 0 && T::planes == 3;        // fp32: the exponentials take the logits' registers
     extern __shared__ uint32_t mask[];            // a bit a column, lowest first
-    __shared__ float part[2 * WAVES];
+    __shared__ double part[2 * WAVES];
     __shared__ int32_t listed[kMostListed];
     __shared__ Listed shared;
     OverRow<WAVES> over{part};
@@ -67,19 +68,23 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
     __syncthreads();
     if (lists) {
         // an entry whose column was listed before is none
-        for (int i = 0; i < a.k; i++) {
-            const int32_t other = listed[i];
+        bool again = false;
 #pragma unroll
-            for (int h = 0; h < 2; h++)
-                if (i < lane + 64 * h && other == column[h]) column[h] = -1;
-        }
+        for (int h = 0; h < 2; h++)
+            if (column[h] >= 0) again |= atomicOr(&mask[column[h] / 32], 1u << (column[h] % 32)) >> (column[h] % 32) & 1;
+        if (__any(again))
+            for (int i = 0; i < a.k; i++) {
+                const int32_t other = listed[i];
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+                    if (i < lane + 64 * h && other == column[h]) column[h] = -1;
+            }
         float t[2] = {-INFINITY, -INFINITY}, most = -INFINITY, count = 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; h++)
             if (column[h] >= 0) {
                 t[h] = a.value[row * a.k + lane + 64 * h] * a.per_T;
                 logit[h] = T::widen(((const E *)a.z)[row * a.ldz + column[h]]);
-                atomicOr(&mask[column[h] / 32], 1u << (column[h] % 32));
                 count += 1.0f;
                 most = fmaxf(most, logit[h]);
             }
@@ -110,37 +115,64 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
         return;
     }
 
-    const auto listed_of = [&](int32_t c) { return (mask[c / 32] >> (c % 32)) & 0xFFu; };
+    const auto listed_of = [&](int32_t c) { return (uint32_t)((((uint64_t)mask[c / 32 + 1] << 32) | mask[c / 32]) >> (c % 32)) & 0xFFu; };
     const float scale = a.per_T * kLog2e;
     float m = -INFINITY, s = 0.0f;
     if constexpr (PACKS > 0) {
-        z.hide_held(listed_of);
-        z.each(listed_of, [&](const Eight &v, int32_t, int32_t) {
+        z.hide_held(listed_of, [&](const Eight &v) {
 #pragma unroll
             for (int i = 0; i < 8; i++) m = fmaxf(m, v.v[i]);
         });
         m = over.most(m);
-        const float from = fmaxf(m, kLowest);
-        z.each(listed_of, [&](const Eight &v, int32_t, int32_t) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) s += __builtin_amdgcn_exp2f((v.v[i] - from) * scale);
-        });
-        s = over.sum(s);
     } else {
         // the largest so far and the sum from it on
-        z.each(listed_of, [&](const Eight &v, int32_t, int32_t) {
+        float from = kLowest;
+        z.each(listed_of, [&](const Eight &v, int32_t, uint32_t) {
             float next = m;
 #pragma unroll
             for (int i = 0; i < 8; i++) next = fmaxf(next, v.v[i]);
-            const float from = fmaxf(next, kLowest);
-            s *= __builtin_amdgcn_exp2f((m - from) * scale);
+            if (next > m) {
+                s *= __builtin_amdgcn_exp2f((m - next) * scale);
+                m = from = next;
+            }
 #pragma unroll
             for (int i = 0; i < 8; i++) s += __builtin_amdgcn_exp2f((v.v[i] - from) * scale);
-            m = next;
         });
         const float own = m;
         m = over.most(m);
         s = over.sum(s * __builtin_amdgcn_exp2f((own - fmaxf(m, kLowest)) * scale));
+    }
+    Powers powers(scale, fmaxf(m, kLowest));
+    if constexpr (PACKS > 0) {
+        if (powers.far()) {                       // (the same for all threads)
+            z.subtract(powers.from);
+            powers = Powers(scale, 0.0f);
+        }
+        z.whole();
+        PackSum sum;
+        const auto add = [&](const Eight &e) {
+            sum.add(((e.v[0] + e.v[1]) + (e.v[2] + e.v[3])) + ((e.v[4] + e.v[5]) + (e.v[6] + e.v[7])));
+        };
+        if constexpr (kept) {
+#pragma unroll
+            for (int i = 0; i < PACKS; i++) {
+                Eight e;
+#pragma unroll
+                for (int k = 0; k < 8; k++) {
+                    e.v[k] = powers(__uint_as_float(z.held[i][k]));
+                    z.held[i][k] = __float_as_uint(e.v[k]);
+                }
+                add(e);
+            }
+        } else {
+            z.each(listed_of, [&](const Eight &v, int32_t, uint32_t) {
+                Eight e;
+#pragma unroll
+                for (int i = 0; i < 8; i++) e.v[i] = powers(v.v[i]);
+                add(e);
+            });
+        }
+        s = over.sum(sum) * powers.lost();
     }
 
     // all relative to the row's largest logit
@@ -171,14 +203,14 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
     }
     if (!a.dz) return;
     const float of_rest = list.p_rest == 0.0f || s == 0.0f ? 0.0f : list.p_rest / s;
-    const float C = factor * a.per_T * (others_exp / total - of_rest);
+    const float C = factor * a.per_T * (others_exp / total - of_rest) * (PACKS > 0 ? powers.lost() : 1.0f);
     E *dz = (E *)a.dz + row * a.lddz;
-    z.each(listed_of, [&](const Eight &v, int32_t c, int32_t left) {
-        if (left <= 0) return;
+    z.each(listed_of, [&](const Eight &v, int32_t c, uint32_t valid) {
+        if (PACKS > 0 && !valid) return;
         Eight d;
 #pragma unroll
-        for (int i = 0; i < 8; i++) d.v[i] = C * __builtin_amdgcn_exp2f((v.v[i] - from) * scale);
-        store_eight<T>(dz + c, d, left);
+        for (int i = 0; i < 8; i++) d.v[i] = C * (kept ? v.v[i] : PACKS > 0 ? powers(v.v[i]) : powers.difference(v.v[i]));
+        z.store(dz + c, d, valid);
     });
     __syncthreads();                              // the list's columns are written over
     if (lists)
@@ -187,10 +219,31 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
             if (column[h] >= 0) dz[column[h]] = narrow<T>(gradient[h]);
 }
 
+// Wavefronts of a row and packs that a lane holds of it: launch(waves, packs), packs 0 where the row is more than the registers hold.
+template <class T, class F>
+int by_columns(int64_t columns, int64_t rows, F launch)
+{
+    using std::integral_constant;
+    const int64_t packs = (columns + 7) / 8;
+#ifdef VW
+    return launch(integral_constant<int, VW>(), integral_constant<int, VP>());
+#endif
+    const bool few = rows <= 256;
+    if (packs <= 64) return launch(integral_constant<int, 1>(), integral_constant<int, 1>());
+    if (packs <= 128) return launch(integral_constant<int, 1>(), integral_constant<int, 2>());
+    if (packs <= 256 && !few) return launch(integral_constant<int, 2>(), integral_constant<int, 2>());
+    if (packs <= 512) return few ? launch(integral_constant<int, 4>(), integral_constant<int, 2>()) : launch(integral_constant<int, 2>(), integral_constant<int, 4>());
+    if (packs <= 1024) return launch(integral_constant<int, 4>(), integral_constant<int, 4>());
+    if (packs <= 2048) return launch(integral_constant<int, 8>(), integral_constant<int, 4>());
+    if (packs <= 4096) return few ? launch(integral_constant<int, 16>(), integral_constant<int, 4>()) : launch(integral_constant<int, 8>(), integral_constant<int, 8>());
+    if (packs <= 8192 && T::planes == 3) return launch(integral_constant<int, 16>(), integral_constant<int, 8>());
+    return launch(integral_constant<int, 16>(), integral_constant<int, 0>());
+}
+
 template <class T>
 int run_distill(const DistillArgs &a, int64_t rows, hipStream_t st)
 {
-    return by_columns<T>(a.columns, [&](auto waves, auto packs) -> int {
+    return by_columns<T>(a.columns, rows, [&](auto waves, auto packs) -> int {
         constexpr int W = decltype(waves)::value, P = decltype(packs)::value;
         if (!fits_launch((uint64_t)rows * 64 * W)) return CCDC_ESIZE;
         k_distill<T, W, P><<<(uint32_t)rows, 64 * W, a.mask_bytes, st>>>(a);
@@ -217,7 +270,7 @@ int ccdc_distill(const ccdc_block_t *b, int64_t rows, int64_t columns, const voi
     for (const void *p : {(const void *)index, (const void *)value, (const void *)rest, (const void *)weight, (const void *)loss})
         if (!aligned(p, 4)) return CCDC_EINVAL;
     if (columns > kMostColumns) return CCDC_ESIZE;
-    const DistillArgs a{z, index, value, rest, weight, loss, dz, ldz, lddz, (int32_t)columns, k, (int32_t)((columns + 31) / 32 * 4), per_T,
+    const DistillArgs a{z, index, value, rest, weight, loss, dz, ldz, lddz, (int32_t)columns, k, (int32_t)((columns / 32 + 2) * 4), per_T,
                         (float)scale};
     CCDC_BY_ELEM(b, (run_distill<T>(a, rows, (hipStream_t)stream)));
 }

@@ -36,8 +36,8 @@ template <class T, int WAVES, int PACKS>
 __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
 {
     constexpr int THREADS = 64 * WAVES, DIGITS = 16 / WAVES, ROUNDS = std::is_same<T, ElemBF16>::value ? 4 : 5;
-    constexpr int kRoom = WAVES <= 2 ? THREADS * PACKS * 8 : 2048;      // of the list
-    __shared__ float part[2 * WAVES];
+    constexpr int kRoom = WAVES == 1 ? 256 : WAVES <= 4 ? 1024 : 2048;  // of the list
+    __shared__ double part[2 * WAVES];
     __shared__ uint32_t largest[THREADS];
     __shared__ int32_t counts[2][16];
     __shared__ uint64_t found[kRoom];
@@ -49,57 +49,78 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     const auto none = [](int32_t) { return 0u; };
     Row<T, WAVES, PACKS> z;
     z.load(a.z, row * a.ldz, a.columns);
-    z.hide_held(none);
-
-    float most = -INFINITY;
-    z.each(none, [&](const Eight &v, int32_t, int32_t) {
+    float most = -INFINITY, pack_most[PACKS ? PACKS : 1];
+    const auto most_of = [&](const Eight &v) {
+        float pack = v.v[0];
 #pragma unroll
-        for (int i = 0; i < 8; i++) most = fmaxf(most, v.v[i]);
-    });
-    const uint32_t own = ordered(most);
-    largest[threadIdx.x] = own;
-    if (threadIdx.x == 0) used = 0, last = 0;
-    __syncthreads();
-    uint32_t all[WAVES], bound = 0;
-#pragma unroll
-    for (int i = 0; i < WAVES; i++) all[i] = largest[i * 64 + lane];
-#pragma unroll
-    for (int round = 0; round < ROUNDS; round++) {
-        const int shift = 28 - 4 * round;
-#pragma unroll
-        for (int d = 0; d < DIGITS; d++) {
-            const int digit = wave * DIGITS + d;
-            const uint32_t from = bound | (uint32_t)digit << shift;
-            int count = 0;
-#pragma unroll
-            for (int i = 0; i < WAVES; i++) count += __popcll(__ballot(all[i] >= from));
-            if (lane == 0) counts[round % 2][digit] = count;
-        }
-        __syncthreads();
-        const uint32_t reach = (uint32_t)__ballot(lane < 16 && counts[round % 2][lane % 16] >= a.k) | 1u;
-        bound |= (uint32_t)(31 - __builtin_clz(reach)) << shift;
-    }
-    bound = max(bound, 1u);
-
-    const auto collect = [&](auto wanted) {
-        z.each(none, [&](const Eight &v, int32_t c, int32_t) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const uint32_t key = ordered(v.v[i]);
-                if (wanted(key, c + i)) {
-                    const int at = atomicAdd(&used, 1);
-                    if (at < kRoom) found[at] = (uint64_t)key << 32 | (0xFFFFFFFFu - (uint32_t)(c + i));
-                }
-            }
-        });
+        for (int i = 1; i < 8; i++) pack = fmaxf(pack, v.v[i]);
+        most = fmaxf(most, pack);
+        return pack;
     };
-    if (own >= bound) collect([&](uint32_t key, int32_t) { return key >= bound; });
+    if constexpr (PACKS > 0) {
+        int i = 0;
+        z.hide_held(none, [&](const Eight &v) { pack_most[i++] = most_of(v); });
+    } else {
+        z.each(none, [&](const Eight &v, int32_t, uint32_t) { most_of(v); });
+    }
+    const uint32_t own = ordered(most);
+    uint32_t bound = 0;
+    if constexpr (WAVES == 1) {
+#pragma unroll
+        for (int bit = 31; bit > 31 - 4 * ROUNDS; bit--) {
+            const uint32_t next = bound | 1u << bit;
+            if ((int)__popcll(__ballot(own >= next)) >= a.k) bound = next;
+        }
+        if (threadIdx.x == 0) used = 0, last = 0;
+        __syncthreads();
+    } else {
+        largest[threadIdx.x] = own;
+        if (threadIdx.x == 0) used = 0, last = 0;
+        __syncthreads();
+        uint32_t all[WAVES];
+#pragma unroll
+        for (int i = 0; i < WAVES; i++) all[i] = largest[i * 64 + lane];
+#pragma unroll
+        for (int round = 0; round < ROUNDS; round++) {
+            const int shift = 28 - 4 * round;
+#pragma unroll
+            for (int d = 0; d < DIGITS; d++) {
+                const int digit = wave * DIGITS + d;
+                const uint32_t from = bound | (uint32_t)digit << shift;
+                int count = 0;
+#pragma unroll
+                for (int i = 0; i < WAVES; i++) count += __popcll(__ballot(all[i] >= from));
+                if (lane == 0) counts[round % 2][digit] = count;
+            }
+            __syncthreads();
+            const uint32_t reach = (uint32_t)__ballot(lane < 16 && counts[round % 2][lane % 16] >= a.k) | 1u;
+            bound |= (uint32_t)(31 - __builtin_clz(reach)) << shift;
+        }
+    }
+    // the same as a number: at least the lowest, so that -infinity and NaNs stay out
+    const float least_wanted = bound > 0x00800000u ? value_of(bound) : kLowest;
+
+    const auto put = [&](float v, int32_t c) {
+        const int to = atomicAdd(&used, 1);
+        if (to < kRoom) found[to] = (uint64_t)ordered(v) << 32 | (0xFFFFFFFFu - (uint32_t)c);
+    };
+    if (most >= least_wanted) {
+        int i = 0;
+        z.each(none, [&](const Eight &v, int32_t c, uint32_t) {
+            bool any = true;
+            if constexpr (PACKS > 0) any = pack_most[i++] >= least_wanted;
+            if (any)
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if (v.v[e] >= least_wanted) put(v.v[e], c + e);
+        });
+    }
     __syncthreads();
     int32_t n = used;
     if (n > kRoom) {                              // (the same for all threads)
         const auto count = [&](auto wanted) {
             float sum = 0.0f;
-            z.each(none, [&](const Eight &v, int32_t c, int32_t) {
+            z.again().each(none, [&](const Eight &v, int32_t c, uint32_t) {
 #pragma unroll
                 for (int i = 0; i < 8; i++) sum += wanted(ordered(v.v[i]), c + i) ? 1.0f : 0.0f;
             });
@@ -118,7 +139,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
         __syncthreads();
         if (threadIdx.x == 0) used = 0;
         __syncthreads();
-        collect([&](uint32_t v, int32_t c) { return v > key || (v == key && (uint32_t)c <= column); });
+        z.again().each(none, [&](const Eight &v, int32_t c, uint32_t) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const uint32_t one = ordered(v.v[i]);
+                if (one > key || (one == key && (uint32_t)(c + i) <= column)) put(v.v[i], c + i);
+            }
+        });
         __syncthreads();
         n = used;
     }
@@ -138,25 +165,38 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     }
     if (!a.rest) return;
     __syncthreads();
-    // What is not listed is at most the last that is: that is what it is summed from, and where so little is left of it that fp32 would
-    // lose it, its own largest.
+    // What is not listed is at most the last that is, which is what it is summed from.  All columns are, none as more than that last: the
+    // k that are listed are then ones, and where half of the sum is left without them it has lost a bit.  Else the listed ones are left
+    // out one by one, and where fp32 has nothing of the others so far below the list, it is from their own largest.
     const uint64_t kth = last;
     const float least = kth ? value_of((uint32_t)(kth >> 32)) : -INFINITY, scale = a.per_T * kLog2e;
     const int32_t column = kth ? (int32_t)(0xFFFFFFFFu - (uint32_t)kth) : -1;
     const auto not_listed = [&](float v, int32_t c) { return v > least || (v == least && c <= column) ? -INFINITY : v; };
-    float from = fmaxf(least, kLowest);
-    const auto sum_from = [&] {
-        float sum = 0.0f;
-        z.each(none, [&](const Eight &v, int32_t c, int32_t) {
+    float from = fmaxf(least, kLowest), sum = 0.0f;
+    const Powers powers(scale, from);
+    const auto sum_of = [&](auto &row, auto term) {
+        PackSum sum;
+        row.each(none, [&](const Eight &v, int32_t c, uint32_t) {
+            float e[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) sum += __builtin_amdgcn_exp2f((not_listed(v.v[i], c + i) - from) * scale);
+            for (int i = 0; i < 8; i++) e[i] = term(v.v[i], c + i);
+            sum.add(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
         });
         return over.sum(sum);
     };
-    float sum = sum_from();
-    if (sum < 1e-30f) {                           // (the same for all threads)
+    if (kth && !powers.far()) {
+        sum = sum_of(z, [&](float v, int32_t) { return powers(v > least ? least : v); });
+        const float listed = (float)a.k * powers(least);
+        sum = sum - listed < listed ? 0.0f : (sum - listed) * powers.lost();
+    }
+    auto again = z.again();
+    const auto sum_from = [&] {
+        return sum_of(again, [&](float v, int32_t c) { return __builtin_amdgcn_exp2f((not_listed(v, c) - from) * scale); });
+    };
+    if (sum == 0.0f) sum = sum_from();            // (the same for all threads)
+    if (sum < 1e-30f) {
         float own_most = -INFINITY;
-        z.each(none, [&](const Eight &v, int32_t c, int32_t) {
+        again.each(none, [&](const Eight &v, int32_t c, uint32_t) {
 #pragma unroll
             for (int i = 0; i < 8; i++) own_most = fmaxf(own_most, not_listed(v.v[i], c + i));
         });
@@ -166,10 +206,33 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     if (threadIdx.x == 0) a.rest[row] = from * a.per_T + logf(sum);
 }
 
+// As distill.hip's.
+template <class T, class F>
+int by_columns(int64_t columns, int64_t rows, F launch)
+{
+    using std::integral_constant;
+    const int64_t packs = (columns + 7) / 8;
+#ifdef VW
+    return launch(integral_constant<int, VW>(), integral_constant<int, VP>());
+#endif
+    const bool few = rows <= 256;
+    if (packs <= 64) return launch(integral_constant<int, 1>(), integral_constant<int, 1>());
+    if (packs <= 128) return launch(integral_constant<int, 1>(), integral_constant<int, 2>());
+    if (packs <= 256 && !few) return launch(integral_constant<int, 1>(), integral_constant<int, 4>());
+    if (packs <= 512) return few ? launch(integral_constant<int, 4>(), integral_constant<int, 2>()) : launch(integral_constant<int, 2>(), integral_constant<int, 4>());
+    if (packs <= 1024) return launch(integral_constant<int, 4>(), integral_constant<int, 4>());
+    if (packs <= 2048) return few ? launch(integral_constant<int, 8>(), integral_constant<int, 4>()) : launch(integral_constant<int, 4>(), integral_constant<int, 8>());
+    if (packs <= 4096) return few ? launch(integral_constant<int, 16>(), integral_constant<int, 4>()) : launch(integral_constant<int, 8>(), integral_constant<int, 8>());
+    if (packs <= 8192) return few || T::planes == 3 ? launch(integral_constant<int, 16>(), integral_constant<int, 8>()) : launch(integral_constant<int, 8>(), integral_constant<int, T::planes == 1 ? 16 : 8>());
+    if constexpr (T::planes == 1)
+        if (packs <= 16384) return launch(integral_constant<int, 16>(), integral_constant<int, 16>());
+    return launch(integral_constant<int, 16>(), integral_constant<int, 0>());
+}
+
 template <class T>
 int run_top(const TopArgs &a, int64_t rows, hipStream_t st)
 {
-    return by_columns<T>(a.columns, [&](auto waves, auto packs) -> int {
+    return by_columns<T>(a.columns, rows, [&](auto waves, auto packs) -> int {
         constexpr int W = decltype(waves)::value, P = decltype(packs)::value;
         if (!fits_launch((uint64_t)rows * 64 * W)) return CCDC_ESIZE;
         k_top<T, W, P><<<(uint32_t)rows, 64 * W, 0, st>>>(a);

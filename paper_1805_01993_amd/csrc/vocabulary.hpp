@@ -24,29 +24,60 @@ __device__ __forceinline__ float wave_most(float v)
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+// exp((v - from) / T) as a power of two, in one product and sum: 2^(v scale - K) with K = from scale rounded.  What K is off by is
+// exact as a product and sum again, below one while K is below 2^24, and `lost` undoes it in a sum of these.  Rows further from zero
+// (those of which the lowest number of the type is the largest, say) are `far`: there the difference is taken first.
+struct Powers {
+    float scale, from, K;
+    __device__ __forceinline__ Powers(float scale, float from) : scale(scale), from(from), K(from * scale) {}
+    __device__ __forceinline__ bool far() const { return !(fabsf(K) < 16777216.0f); }
+    __device__ __forceinline__ float operator()(float v) const { return __builtin_amdgcn_exp2f(fmaf(v, scale, -K)); }
+    __device__ __forceinline__ float lost() const { return __builtin_amdgcn_exp2f(-fmaf(from, scale, -K)); }
+    __device__ __forceinline__ float difference(float v) const { return __builtin_amdgcn_exp2f((v - from) * scale); }
+};
+
+// A sum of the packs of a row that is the same whatever thread has which of them: in 64 bits, of numbers rounded to 2^-32, which is exact
+// up to 2^21 (a pack is at most 8 exponentials of at most 2^(1/2), of 2^17 packs).  The roundings are 2^-33 a pack where the sum is one
+// or more.  Four instructions a pack of eight.
+struct PackSum {
+    double sum = 0.0;
+    __device__ __forceinline__ void add(float pack)
+    {
+        constexpr double kRound = 1.5 * 1048576.0;            // numbers from 2^20 to 2^21 are whole 2^-32
+        sum += ((double)pack + kRound) - kRound;
+    }
+};
+
 // Sums and largest values over a row's threads, wavefronts by LDS in their order.  Parts of the LDS in turn, so that one barrier is
 // enough: who writes a part again has met the others since they read it.
 template <int WAVES>
 struct OverRow {
-    float *part;                                  // [2][WAVES]
+    double *part;                                 // [2][WAVES]
     int at = 0;
 
-    template <class F>
-    __device__ __forceinline__ float join(float v, F both)
+    template <class V, class F>
+    __device__ __forceinline__ V join(V v, F both)
     {
         if constexpr (WAVES == 1) return v;
-        float *slot = part + at;
+        double *slot = part + at;
         at = WAVES - at;
         if (threadIdx.x % 64 == 0) slot[threadIdx.x / 64] = v;
         __syncthreads();
-        v = slot[0];
+        v = (V)slot[0];
 #pragma unroll
-        for (int i = 1; i < WAVES; i++) v = both(v, slot[i]);
+        for (int i = 1; i < WAVES; i++) v = both(v, (V)slot[i]);
         return v;
     }
     __device__ __forceinline__ float sum(float v)
     {
         return join(wave_sum(v), [](float a, float b) { return a + b; });
+    }
+    __device__ __forceinline__ float sum(const PackSum &s)
+    {
+        double v = s.sum;
+#pragma unroll
+        for (int step = 1; step < 64; step *= 2) v += __shfl_xor(v, step);
+        return (float)join(v, [](double a, double b) { return a + b; });
     }
     __device__ __forceinline__ float most(float v)
     {
@@ -54,24 +85,25 @@ struct OverRow {
     }
 };
 
-// The bits of a pack's columns that are past the row's end, `left` columns on.
-__device__ __forceinline__ uint32_t past(int32_t left) { return left >= 8 ? 0u : 0xFFu << max(left, 0) & 0xFFu; }
-
-// A pack with -infinity where a bit is set.
+// Word w of a pack with -infinity where a bit is set (16-bit elements: two a word).
 template <class T>
-__device__ __forceinline__ Raw8<T> hide(Raw8<T> raw, uint32_t bits)
+__device__ __forceinline__ uint32_t hide_word(uint32_t word, uint32_t bits, int w)
 {
-    using E = typename T::elem;
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        if constexpr (sizeof(E) == 4) raw.p.v[i] = bits >> i & 1 ? -INFINITY : raw.p.v[i];
-        else raw.p.v[i] = bits >> i & 1 ? (E)(std::is_same<T, ElemF16>::value ? 0xFC00 : 0xFF80) : raw.p.v[i];
+    if constexpr (sizeof(typename T::elem) == 4) {
+        const uint32_t mask = (uint32_t)__builtin_amdgcn_sbfe((int)bits, w, 1);
+        return (word & ~mask) | (0xFF800000u & mask);
+    } else {
+        constexpr uint32_t kNone = std::is_same<T, ElemF16>::value ? 0xFC00FC00u : 0xFF80FF80u;
+        const uint32_t low = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 2 * w, 1), high = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 2 * w + 1, 1);
+        const uint32_t mask = (low & 0xFFFFu) | (high & 0xFFFF0000u);
+        return (word & ~mask) | (kNone & mask);
     }
-    return raw;
 }
 
-// The packs of eight columns that a thread has of a row: (its place) + i * (threads).  PACKS > 0: as many at the most, held in registers as
-// loaded; 0: any number, read whenever they are asked for.  What is hidden, and what is past the row's end, is -infinity.
+// A row in packs of eight columns.  The last is read as the row's last eight, and what the one before has too is hidden: every read
+// is of eight columns in the row, also those of lanes past its end, and none takes a way of its own.
+// A thread has packs (its place) + i * (threads).  PACKS > 0: as many at the most, held in registers as loaded; 0: any number, read
+// whenever they are asked for.  What is hidden is -infinity.
 template <class T, int WAVES, int PACKS>
 struct Row {
     using E = typename T::elem;
@@ -80,77 +112,145 @@ struct Row {
     int32_t columns;
     uint32_t held[PACKS ? PACKS : 1][kWords];
 
+    struct Pack8 {
+        int32_t start;                    // first column that is read
+        uint32_t valid;                   // of the eight: those that are this pack's
+    };
+    __device__ __forceinline__ Pack8 pack_of(int32_t j) const
+    {
+        const int32_t first = j * 8, start = max(min(first, columns - 8), 0), from = first - start;
+        return {start, from < 8 ? (1u << min(columns - start, 8)) - (1u << from) : 0u};
+    }
+    __device__ __forceinline__ void read(uint32_t (&words)[kWords], int32_t start) const
+    {
+        if (columns >= 8) {               // (the same for all)
+            constexpr int W = 16 / sizeof(E);
+            using P = Pack<E, W>;
+#pragma unroll
+            for (int h = 0; h < 8 / W; h++) {
+                const P q = load_pack_any<true, P, E>(p + start + h * W);
+                __builtin_memcpy(&words[h * 4], &q, sizeof q);
+            }
+        } else {
+            const Raw8<T> raw = load_raw<T>(p, columns);
+            __builtin_memcpy(words, &raw, sizeof raw);
+        }
+    }
+    // Not held, for what few rows need: the same row read again.
+    __device__ __forceinline__ Row<T, WAVES, 0> again() const
+    {
+        Row<T, WAVES, 0> row;
+        row.p = p, row.columns = columns;
+        return row;
+    }
     __device__ __forceinline__ void load(const void *base, int64_t at, int32_t of)
     {
         p = (const E *)base + at;
         columns = of;
 #pragma unroll
+        for (int i = 0; i < PACKS; i++) read(held[i], pack_of(fresh((int32_t)threadIdx.x + i * kThreads)).start);
+    }
+    // Eight numbers, widened.  The compiler does not see that a held pack is what it was in another pass, or it would keep all 16-bit
+    // numbers widened.
+    __device__ __forceinline__ static Eight wide(const uint32_t (&from)[kWords], uint32_t shift, uint32_t mask)
+    {
+        Eight v;
+        if constexpr (std::is_same<T, ElemBF16>::value) {
+#pragma unroll
+            for (int w = 0; w < 4; w++) v.v[2 * w] = __uint_as_float(from[w] << shift), v.v[2 * w + 1] = __uint_as_float(from[w] & mask);
+        } else {
+            uint32_t words[kWords];
+#pragma unroll
+            for (int w = 0; w < kWords; w++) {
+                words[w] = from[w];
+                if (T::planes == 1) asm volatile("" : "+v"(words[w]));
+            }
+            Raw8<T> raw;
+            __builtin_memcpy(&raw, words, sizeof raw);
+            v = widen(raw);
+        }
+        return v;
+    }
+    // Registers of whole words from here on, whatever ways lead here.
+    __device__ __forceinline__ void whole()
+    {
+#pragma unroll
+        for (int i = 0; i < PACKS; i++)
+#pragma unroll
+            for (int w = 0; w < kWords; w++) asm volatile("" : "+v"(held[i][w]));
+    }
+    // Hides the columns of held packs that hidden(first of eight columns) has bits of, and f(values) for each pack.
+    template <class H, class F>
+    __device__ __forceinline__ void hide_held(H hidden, F f)
+    {
+        const uint32_t shift = fresh_uniform(16u), mask = fresh_uniform(0xFFFF0000u);
+        whole();
+#pragma unroll
         for (int i = 0; i < PACKS; i++) {
-            const int32_t c = fresh((int32_t)threadIdx.x + i * kThreads) * 8;
-            Raw8<T> raw = {};
-            if (c < columns) raw = load_raw<T>(p + c, columns - c);
+            const Pack8 pack = pack_of(fresh((int32_t)threadIdx.x + i * kThreads));
+            const uint32_t bits = hidden(pack.start) | ~pack.valid;
+#pragma unroll
+            for (int w = 0; w < kWords; w++) held[i][w] = hide_word<T>(held[i][w], bits, w);
+            f(wide(held[i], shift, mask));
+        }
+        whole();
+    }
+    // All numbers less what they have in common.  Exact where it matters: of rows so far from zero (Powers) the differences that are no
+    // whole few steps of the type are exponentials of zero.
+    __device__ __forceinline__ void subtract(float from)
+    {
+#pragma unroll
+        for (int i = 0; i < PACKS; i++) {
+            Raw8<T> raw;
+            __builtin_memcpy(&raw, held[i], sizeof raw);
+#pragma unroll
+            for (int e = 0; e < 8; e++) raw.p.v[e] = narrow<T>(T::widen(raw.p.v[e]) - from);
             __builtin_memcpy(held[i], &raw, sizeof raw);
         }
     }
-    // Pack i as held; the compiler sees another number each time, or it would keep all packs widened from one pass to the next.
-    __device__ __forceinline__ Raw8<T> pack(int i)
-    {
-#pragma unroll
-        for (int w = 0; w < kWords; w++) asm volatile("" : "+v"(held[i][w]));
-        Raw8<T> raw;
-        __builtin_memcpy(&raw, held[i], sizeof raw);
-        return raw;
-    }
-    // Hides the columns that hidden(first column of a pack) has bits of.
-    template <class H>
-    __device__ __forceinline__ void hide_held(H hidden)
-    {
-#pragma unroll
-        for (int i = 0; i < PACKS; i++) {
-            const int32_t c = fresh((int32_t)threadIdx.x + i * kThreads) * 8;
-            const Raw8<T> raw = hide<T>(pack(i), c < columns ? hidden(c) | past(columns - c) : 0xFFu);
-            __builtin_memcpy(held[i], &raw, sizeof raw);
-        }
-    }
-    // f(values, first column, columns of them in the row, which may be none) for each pack.
+    // f(values, first of their eight columns, which of them are this pack's) for each pack; those that are read now are hidden now.
     template <class H, class F>
     __device__ __forceinline__ void each(H hidden, F f)
     {
+        const uint32_t shift = fresh_uniform(16u), mask = fresh_uniform(0xFFFF0000u);
         if constexpr (PACKS > 0) {
 #pragma unroll
             for (int i = 0; i < PACKS; i++) {
-                const int32_t c = fresh((int32_t)threadIdx.x + i * kThreads) * 8;
-                f(widen(pack(i)), c, columns - c);
+                const Pack8 pack = pack_of(fresh((int32_t)threadIdx.x + i * kThreads));
+                f(wide(held[i], shift, mask), pack.start, pack.valid);
+                // one after the other: with packs interleaved a row of eight takes half as many registers again
+                __builtin_amdgcn_sched_barrier(0);
             }
         } else {
             // two packs on their way at a time
-            for (int32_t c = (int32_t)threadIdx.x * 8; c < columns; c += 2 * kThreads * 8) {
-                const int32_t next = c + kThreads * 8;
-                const Raw8<T> one = load_raw<T>(p + c, columns - c);
-                const Raw8<T> two = next < columns ? load_raw<T>(p + next, columns - next) : Raw8<T>{};
-                f(widen(hide<T>(one, hidden(c) | past(columns - c))), c, columns - c);
-                if (next < columns) f(widen(hide<T>(two, hidden(next) | past(columns - next))), next, columns - next);
+            const int32_t packs = (columns + 7) / 8;
+            for (int32_t j = (int32_t)threadIdx.x; j < packs; j += 2 * kThreads) {
+                const Pack8 pack[2] = {pack_of(j), pack_of(j + kThreads)};
+                uint32_t words[2][kWords];
+#pragma unroll
+                for (int h = 0; h < 2; h++) read(words[h], pack[h].start);
+#pragma unroll
+                for (int h = 0; h < 2; h++) {
+                    const uint32_t bits = (hidden(pack[h].start) | ~pack[h].valid) & 0xFFu;
+                    if (bits)             // few packs
+#pragma unroll
+                        for (int w = 0; w < kWords; w++) words[h][w] = hide_word<T>(words[h][w], bits, w);
+                    if (pack[h].valid) f(wide(words[h], shift, mask), pack[h].start, pack[h].valid);
+                }
             }
         }
     }
+    // Writes eight columns from `start` on, those that are valid.
+    static __device__ __forceinline__ void store(E *to, const Eight &v, uint32_t valid)
+    {
+        if (valid == 0xFFu) {
+            store_eight<T>(to, v, 8);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                if (valid >> e & 1) to[e] = narrow<T>(v.v[e]);
+        }
+    }
 };
-
-// Wavefronts of a row and packs that a lane holds of it: launch(waves, packs), packs 0 where the row is more than the registers hold.  Rows
-// of 1024 threads have 128 registers a lane; two such workgroups are on a CU up to four packs, so that one's loads meet the other's
-// sums.
-template <class T, class F>
-int by_columns(int64_t columns, F launch)
-{
-    using std::integral_constant;
-    const int64_t packs = (columns + 7) / 8;
-    if (packs <= 64) return launch(integral_constant<int, 1>(), integral_constant<int, 1>());
-    if (packs <= 128) return launch(integral_constant<int, 2>(), integral_constant<int, 1>());
-    if (packs <= 512) return launch(integral_constant<int, 4>(), integral_constant<int, 2>());
-    if (packs <= 1024) return launch(integral_constant<int, 4>(), integral_constant<int, 4>());
-    if (packs <= 2048) return launch(integral_constant<int, 8>(), integral_constant<int, 4>());
-    if (packs <= 4096) return launch(integral_constant<int, 16>(), integral_constant<int, 4>());
-    if (packs <= 8192) return launch(integral_constant<int, 16>(), integral_constant<int, 8>());
-    return launch(integral_constant<int, 16>(), integral_constant<int, 0>());
-}
 
 }  // namespace ccdc

@@ -232,17 +232,26 @@ def test_top_of_equal_and_masked_logits(blocks, mode, columns):
     check_top(blocks[mode], z, 1, 0.5, with_rest=False)
 
 
-def test_top_is_the_same_every_time_and_in_any_batch(blocks):
-    z = noise(4, 40, 33000, std=2.0).to(torch.bfloat16).cuda()
-    made = []
-    for rows in (range(40), range(40), [7], [39, 7]):
-        part = z[list(rows)]
-        index, value = (torch.zeros(len(part), 50, dtype=t, device="cuda") for t in (torch.int32, torch.float32))
-        rest = torch.zeros(len(part), device="cuda")
-        blocks["bf16"].top(part, index, value, rest=rest)
-        made.append((list(rows), index, value, rest))
-    for rows, index, value, rest in made[1:]:
-        assert torch.equal(index, made[0][1][rows]) and torch.equal(value, made[0][2][rows]) and torch.equal(rest, made[0][3][rows])
+@pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("columns", [500, 999, 1801, 3501, 8000, 16001, 32001, 50021, 70001])
+def test_a_row_is_the_same_every_time_and_in_any_batch(blocks, mode, columns):
+    """Nodes that store a file make the same bits of its rows, whatever else is in their batches, how many rows they have and what
+    addresses the rows begin at."""
+    block, k, d = blocks[mode], 20, R.DTYPES[mode]
+    z = noise(4, 300, columns, std=2.0).to(d).cuda()
+    whole = None
+    for rows in (list(range(300)), list(range(300)), [7], [299, 7, 120]):
+        part = z[rows].contiguous()
+        new = lambda t, *shape: torch.zeros(shape, dtype=t, device="cuda")  # noqa: E731
+        made = {"index": new(torch.int32, len(rows), k), "value": new(torch.float32, len(rows), k), "rest": new(torch.float32, len(rows)),
+                "loss": new(torch.float32, len(rows)), "dz": new(d, len(rows), columns)}
+        block.top(part, made["index"], made["value"], rest=made["rest"], temperature=1.5)
+        # (the neighbour's answer, so that something is left to learn)
+        index, value = made["index"].roll(3, 1).contiguous(), made["value"].contiguous()
+        block.distill(part, index, value, made["loss"], made["dz"], rest=made["rest"], temperature=1.5)
+        whole = whole or made
+        for name, t in made.items():
+            assert torch.equal(t.view(torch.uint8), whole[name][rows].contiguous().view(torch.uint8)), (name, len(rows))
 
 
 # ------------------------------------------------------------------ distillation
