@@ -109,7 +109,7 @@ int ccdc_packed_product(const ccdc_block_t *b, int64_t rows, int64_t outputs, in
     const int32_t ld = (int32_t)packed_columns(columns);
     const Product8Args a{(const uint8_t *)W, (const uint8_t *)x, (const uint8_t *)W_scale, (const uint8_t *)x_scale, ld,
                          (int32_t)packed_scales(columns), (int32_t)outputs, (int32_t)rows, ld / 128, 0, 0, y, ldy};
-    return rows <= kFewRows8 ? few_product8(b, a, (hipStream_t)stream) : tiled_product8(b, a, (hipStream_t)stream);
+    return few_rows8(b, a) ? few_product8(b, a, (hipStream_t)stream) : tiled_product8(b, a, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -45,8 +45,8 @@ __device__ __forceinline__ Wide8 wide(int low, int high, float scale)
     return Wide8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// The products of at most kFewRows8 rows (few8.hip) and of more (product8.hip).
-constexpr int64_t kFewRows8 = 64;
+// The products of a few rows (few8.hip), where they are the faster, and of more (product8.hip).
+bool few_rows8(const ccdc_block_t *b, const Product8Args &a);
 int few_product8(const ccdc_block_t *b, const Product8Args &a, hipStream_t st);
 int tiled_product8(const ccdc_block_t *b, const Product8Args &a, hipStream_t st);
 

@@ -6,6 +6,8 @@
 // Bytes lie in LDS as [row][128], a row's packs of 16 in an order of its own (product.hip: what a wavefront reads together is in
 // different banks).  A lane has 32 of a row's 64 k of an instruction, the same ones on both sides, which is all that a
 // product asks for.
+#include <algorithm>
+
 #include "eight.hpp"
 
 namespace {
@@ -319,21 +321,23 @@ int launch(Product8Args a, hipStream_t st)
     return launched();
 }
 
-// Tiles of 256 x 256, one a CU, or of 128 x 128, two, by the rounds of them that the chip's 256 CUs make.
-inline bool large_tiles(const Product8Args &a)
-{
-    const auto rounds = [&](uint32_t size, uint32_t at_once) { return (double)cdiv((uint64_t)cdiv(a.rows_n, size) * cdiv(a.rows_m, size), at_once); };
-    return rounds(256, 256) * 1.75 <= rounds(128, 512);
-}
-
+// The tile by the rounds of them that the chip's 256 CUs make, at what a step of a round took (us; 65 to 8192 rows of 2048 and 4096 columns,
+// 4096 to 11264 outputs, bf16): 256 x 256, one a CU, 1.65; 128 x 128 two a CU 1.2, or one with twice the steps in LDS 0.72; 64 outputs x 128
+// rows, one a CU, 0.59; 64 x 64, two a CU, 0.66, of one 0.5.  333 rows of 2048 x 4160: 9.1 us by 64 x 128, by 128 x 128 11.5; 64 rows of 4096
+// x 11264 16.0 by 64 x 64, 21.4; 1024 rows 56 by the largest, 68 and 74 by 128 x 128.
 template <class T>
 int run_product8(const Product8Args &a, hipStream_t st)
 {
+    const auto tiles = [&](uint32_t n, uint32_t m) { return (uint64_t)cdiv(a.rows_n, n) * cdiv(a.rows_m, m); };
+    const double largest = cdiv(tiles(256, 256), 256) * 1.65, two = cdiv(tiles(128, 128), 512) * 1.2, one = cdiv(tiles(128, 128), 256) * 0.72;
+    const double tall = cdiv(tiles(64, 128), 256) * 0.59, small = tiles(64, 64) <= 256 ? 0.5 : cdiv(tiles(64, 64), 512) * 0.66;
+    const double least = std::min(std::min(small, tall), std::min(one, two));
     if constexpr (T::planes == 1)                     // (in fp32 a large tile's pieces as bfloat16 are more registers than there are)
-        if (large_tiles(a)) return launch<T, 4, 2, 2, 4, 2>(a, st);
-    const uint64_t small = (uint64_t)cdiv(a.rows_n, 128) * cdiv(a.rows_m, 128);
-    if (small > 256) return launch<T, 2, 4, 2, 1, 2>(a, st);
-    return launch<T, 2, 4, 2, 1, 4>(a, st);           // one a CU: with its LDS, more of a tile on its way
+        if (largest <= least) return launch<T, 4, 2, 2, 4, 2>(a, st);
+    if (small == least) return launch<T, 1, 2, 2, 1, 4>(a, st);
+    if (tall == least) return launch<T, 1, 4, 2, 1, 4>(a, st);
+    if (one == least) return launch<T, 2, 4, 2, 1, 4>(a, st);
+    return launch<T, 2, 4, 2, 1, 2>(a, st);
 }
 
 }  // namespace
