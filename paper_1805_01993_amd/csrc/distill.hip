@@ -119,7 +119,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
     const float scale = a.per_T * kLog2e;
     float m = -INFINITY, s = 0.0f;
     if constexpr (PACKS > 0) {
-        z.hide_held(listed_of, [&](const Eight &v) {
+        z.template hide_held<false>(listed_of, [&](const Eight &v) {
 #pragma unroll
             for (int i = 0; i < 8; i++) m = fmaxf(m, v.v[i]);
         });
@@ -156,6 +156,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
         if constexpr (kept) {
 #pragma unroll
             for (int i = 0; i < PACKS; i++) {
+                if (!z.some(i)) continue;
                 Eight e;
 #pragma unroll
                 for (int k = 0; k < 8; k++) {

@@ -40,7 +40,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     __shared__ double part[2 * WAVES];
     __shared__ uint32_t largest[THREADS];
     __shared__ int32_t counts[2][16];
-    __shared__ uint64_t found[kRoom];
+    __shared__ __attribute__((aligned(16))) uint64_t found[kRoom + 8];
     __shared__ int32_t used;
     __shared__ uint64_t last;
     OverRow<WAVES> over{part};
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     const auto none = [](int32_t) { return 0u; };
     Row<T, WAVES, PACKS> z;
     z.load(a.z, row * a.ldz, a.columns);
-    float most = -INFINITY, pack_most[PACKS ? PACKS : 1];
+    float most = -INFINITY, pack_most[PACKS ? PACKS : 1] = {};
     const auto most_of = [&](const Eight &v) {
         float pack = v.v[0];
 #pragma unroll
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     };
     if constexpr (PACKS > 0) {
         int i = 0;
-        z.hide_held(none, [&](const Eight &v) { pack_most[i++] = most_of(v); });
+        z.template hide_held<true>(none, [&](const Eight &v) { pack_most[i++] = most_of(v); });
     } else {
         z.each(none, [&](const Eight &v, int32_t, uint32_t) { most_of(v); });
     }
@@ -150,10 +150,20 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
         n = used;
     }
 
+    // places past the list's end are the lowest, up to whole groups of them that are read together
+    constexpr int kTogether = 8;
+    if ((int)threadIdx.x < kTogether) found[n + threadIdx.x] = 0;
+    __syncthreads();
     for (int i = threadIdx.x; i < n; i += THREADS) {
         const uint64_t mine = found[i];
         int rank = 0;
-        for (int j = 0; j < n; j++) rank += found[j] > mine ? 1 : 0;
+        for (int j = 0; j < n; j += kTogether) {
+            uint64_t other[kTogether];
+#pragma unroll
+            for (int o = 0; o < kTogether; o++) other[o] = found[j + o];
+#pragma unroll
+            for (int o = 0; o < kTogether; o++) rank += other[o] > mine ? 1 : 0;
+        }
         if (rank >= a.k) continue;
         a.index[row * a.k + rank] = (int32_t)(0xFFFFFFFFu - (uint32_t)mine);
         a.value[row * a.k + rank] = value_of((uint32_t)(mine >> 32));

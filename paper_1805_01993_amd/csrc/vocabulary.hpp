@@ -36,6 +36,27 @@ struct Powers {
     __device__ __forceinline__ float difference(float v) const { return __builtin_amdgcn_exp2f((v - from) * scale); }
 };
 
+// As wave_sum of 32 bits (element.hpp).
+__device__ __forceinline__ double wave_sum(double v)
+{
+    const auto moved = [](double x, auto control, auto rows) {
+        const int2 from = __builtin_bit_cast(int2, x);
+        int2 to;
+        to.x = __builtin_amdgcn_update_dpp(0, from.x, decltype(control)::value, decltype(rows)::value, 15, true);
+        to.y = __builtin_amdgcn_update_dpp(0, from.y, decltype(control)::value, decltype(rows)::value, 15, true);
+        return __builtin_bit_cast(double, to);
+    };
+    using std::integral_constant;
+    v += moved(v, integral_constant<int, 0x111>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x112>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x114>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x118>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x142>(), integral_constant<int, 10>());
+    v += moved(v, integral_constant<int, 0x143>(), integral_constant<int, 12>());
+    const int2 all = __builtin_bit_cast(int2, v);
+    return __builtin_bit_cast(double, int2{__builtin_amdgcn_readlane(all.x, 63), __builtin_amdgcn_readlane(all.y, 63)});
+}
+
 // A sum of the packs of a row that is the same whatever thread has which of them: in 64 bits, of numbers rounded to 2^-32, which is exact
 // up to 2^21 (a pack is at most 8 exponentials of at most 2^(1/2), of 2^17 packs).  The roundings are 2^-33 a pack where the sum is one
 // or more.  Four instructions a pack of eight.
@@ -74,10 +95,7 @@ struct OverRow {
     }
     __device__ __forceinline__ float sum(const PackSum &s)
     {
-        double v = s.sum;
-#pragma unroll
-        for (int step = 1; step < 64; step *= 2) v += __shfl_xor(v, step);
-        return (float)join(v, [](double a, double b) { return a + b; });
+        return (float)join(wave_sum(s.sum), [](double a, double b) { return a + b; });
     }
     __device__ __forceinline__ float most(float v)
     {
@@ -136,6 +154,8 @@ struct Row {
             __builtin_memcpy(words, &raw, sizeof raw);
         }
     }
+    // Whether any thread's pack i is in the row.
+    __device__ __forceinline__ bool some(int i) const { return i * kThreads * 8 < columns; }
     // Not held, for what few rows need: the same row read again.
     __device__ __forceinline__ Row<T, WAVES, 0> again() const
     {
@@ -148,7 +168,8 @@ struct Row {
         p = (const E *)base + at;
         columns = of;
 #pragma unroll
-        for (int i = 0; i < PACKS; i++) read(held[i], pack_of(fresh((int32_t)threadIdx.x + i * kThreads)).start);
+        for (int i = 0; i < PACKS; i++)
+            if (some(i)) read(held[i], pack_of(fresh((int32_t)threadIdx.x + i * kThreads)).start);
     }
     // Eight numbers, widened.  The compiler does not see that a held pack is what it was in another pass, or it would keep all 16-bit
     // numbers widened.
@@ -179,21 +200,28 @@ struct Row {
 #pragma unroll
             for (int w = 0; w < kWords; w++) asm volatile("" : "+v"(held[i][w]));
     }
-    // Hides the columns of held packs that hidden(first of eight columns) has bits of, and f(values) for each pack.
-    template <class H, class F>
+    // Hides the columns of held packs that hidden(first of eight columns) has bits of, and f(values) for each pack.  FEW: where only few packs
+    // have any, they alone do it (with many that is a way past half of them, and more registers).
+    template <bool FEW, class H, class F>
     __device__ __forceinline__ void hide_held(H hidden, F f)
     {
         const uint32_t shift = fresh_uniform(16u), mask = fresh_uniform(0xFFFF0000u);
         whole();
 #pragma unroll
         for (int i = 0; i < PACKS; i++) {
+            if (!some(i)) continue;
             const Pack8 pack = pack_of(fresh((int32_t)threadIdx.x + i * kThreads));
-            const uint32_t bits = hidden(pack.start) | ~pack.valid;
+            const uint32_t bits = (hidden(pack.start) | ~pack.valid) & 0xFFu;
+            if (!FEW || bits)
 #pragma unroll
-            for (int w = 0; w < kWords; w++) held[i][w] = hide_word<T>(held[i][w], bits, w);
-            f(wide(held[i], shift, mask));
+                for (int w = 0; w < kWords; w++) held[i][w] = hide_word<T>(held[i][w], bits, w);
+            if constexpr (!FEW) f(wide(held[i], shift, mask));
         }
         whole();
+        if constexpr (FEW)
+#pragma unroll
+            for (int i = 0; i < PACKS; i++)
+                if (some(i)) f(wide(held[i], shift, mask));
     }
     // All numbers less what they have in common.  Exact where it matters: of rows so far from zero (Powers) the differences that are no
     // whole few steps of the type are exponentials of zero.
@@ -216,6 +244,7 @@ struct Row {
         if constexpr (PACKS > 0) {
 #pragma unroll
             for (int i = 0; i < PACKS; i++) {
+                if (!some(i)) continue;
                 const Pack8 pack = pack_of(fresh((int32_t)threadIdx.x + i * kThreads));
                 f(wide(held[i], shift, mask), pack.start, pack.valid);
                 // one after the other: with packs interleaved a row of eight takes half as many registers again
@@ -240,10 +269,21 @@ struct Row {
             }
         }
     }
-    // Writes eight columns from `start` on, those that are valid.
+    // Writes eight columns from `start` on, those that are valid.  Rows that are read again go past the caches, which have then more of
+    // what is read (1500 x 131071 f16 250 -> 233 us).
     static __device__ __forceinline__ void store(E *to, const Eight &v, uint32_t valid)
     {
-        if (valid == 0xFFu) {
+        if (valid == 0xFFu && PACKS == 0) {
+            constexpr int W = 16 / sizeof(E);
+            using P = Pack<E, W>;
+#pragma unroll
+            for (int h = 0; h < 8 / W; h++) {
+                P q;
+#pragma unroll
+                for (int i = 0; i < W; i++) q.v[i] = narrow<T>(v.v[h * W + i]);
+                store_stream_any<P, E>(to + h * W, q);
+            }
+        } else if (valid == 0xFFu) {
             store_eight<T>(to, v, 8);
         } else {
 #pragma unroll

@@ -2,10 +2,12 @@
 shuffle sums it.
 
     python -m paper_1805_01993_amd.train [--nodes 8] [--replication 2] [--width 256] [--hidden 512] [--tokens 64]
-                                         [--steps 20] [--mode bf16] [--dropout 0.1]
+                                         [--steps 20] [--mode bf16] [--dropout 0.1] [--teacher 0]
 
 The block predicts targets from its inputs: n = norm(x), f = feed-forward(n), y = scale x + gate D(norm(f)), loss
-|y - target|^2 / 2 per element.  A step
+|y - target|^2 / 2 per element.  With a teacher, y are logits over `width` symbols, and the loss is a token's distance from the answer of
+a teacher whose weights are packed in 8 bits: its largest logits, as many as --teacher says, and what all others come to
+(ccdc_quantise, ccdc_packed_product, ccdc_top, ccdc_distill).  A step
 
   maps       every file to the gradient of its own tokens: a join, the feed-forward block, a join, and back (ccdc_join_*,
              ccdc_ffn_*); the gradients of one file are its row of V, [W_in | W_out | w_pre | w_post | gate]
@@ -23,15 +25,19 @@ import math
 
 import torch
 
-from .binding import ccdc_block, ccdc_plan
+from .binding import ccdc_block, ccdc_plan, packed_shapes
 
+TEMPERATURE = 2.0
+# From this many rows on the sums of a packed product have one order: a node that has fewer makes the others of nothing.
+ROWS_OF_ONE_ORDER = 65
 TORCH = {"f32": torch.float32, "h32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 
 
 class Trainer:
     """The cluster's plan, the block and its parameters (fp32 masters), and a data set of one token matrix a file."""
 
-    def __init__(self, nodes, replication, width, hidden, tokens, mode="bf16", dropout=0.1, seed=0, residual_scale=0.5):
+    def __init__(self, nodes, replication, width, hidden, tokens, mode="bf16", dropout=0.1, seed=0, residual_scale=0.5,
+                 teacher=0):
         self.width, self.hidden, self.mode, self.dropout, self.scale = width, hidden, mode, dropout, residual_scale
         files = math.comb(nodes, replication)
         self.tokens = [tokens] * files if isinstance(tokens, int) else list(tokens)
@@ -53,6 +59,12 @@ class Trainer:
         self.V = torch.zeros(shapes["V"], dtype=dtype, device="cuda")        # what a row has past the parameters stays zero
         self.X = torch.empty(shapes["X"], dtype=dtype, device="cuda")
         self.Phi = torch.empty(shapes["Phi"], dtype=dtype, device="cuda")
+        self.teacher = teacher
+        if teacher:
+            weights = (4 * torch.randn(width, width, generator=g) / math.sqrt(width)).to(dtype).cuda()
+            q, scale = packed_shapes(width, width)
+            self.packed = torch.empty(q, dtype=torch.uint8, device="cuda"), torch.empty(scale, dtype=torch.uint8, device="cuda")
+            ccdc_block(width, 1, mode).bind([1]).upload().quantise(weights, *self.packed)
         self.every = self._batch(range(files))
 
     def _batch(self, files):
@@ -65,7 +77,25 @@ class Trainer:
         rows = block.tokens
         new = lambda: torch.empty(rows, self.width, dtype=self.x.dtype, device="cuda")  # noqa: E731
         return {"block": block, "first": first, "saved": torch.empty(block.saved_bytes, dtype=torch.uint8, device="cuda"),
-                "n": new(), "f": new(), "y": new(), "df": new(), "dn": new()}
+                "n": new(), "f": new(), "y": new(), "df": new(), "dn": new(), **(self._answers(rows) if self.teacher else {})}
+
+    def _answers(self, rows):
+        """Buffers of the teacher's answers to so many tokens, and of the student's distance from them."""
+        most, new = max(rows, ROWS_OF_ONE_ORDER), lambda dtype, *shape: torch.zeros(shape, dtype=dtype, device="cuda")
+        q, scale = packed_shapes(most, self.width)
+        return {"q": new(torch.uint8, *q), "scale": new(torch.uint8, *scale), "logits": new(self.x.dtype, most, self.width),
+                "index": new(torch.int32, rows, self.teacher), "value": new(torch.float32, rows, self.teacher),
+                "rest": new(torch.float32, rows), "loss": new(torch.float32, rows), "dy": new(self.x.dtype, rows, self.width)}
+
+    def _distance(self, block, s, x):
+        """The loss and, in s["dy"], its gradient at the student's logits s["y"]."""
+        rows = x.shape[0]
+        block.quantise(x, s["q"][:rows], s["scale"][:rows])
+        block.packed_product(s["q"], s["scale"], *self.packed, s["logits"])
+        block.top(s["logits"][:rows], s["index"], s["value"], rest=s["rest"], temperature=TEMPERATURE)
+        block.distill(s["y"], s["index"], s["value"], s["loss"], s["dy"], rest=s["rest"], temperature=TEMPERATURE,
+                      scale=TEMPERATURE * TEMPERATURE)
+        return s["loss"].mean()
 
     def parameters(self):
         """The parameters as the step's products take them."""
@@ -85,12 +115,16 @@ class Trainer:
         s["first"].join_forward(x, None, None, s["n"], w_pre=p["w_pre"])
         block.ffn_forward(s["n"], p["W_in"], p["W_out"], s["f"], saved=s["saved"], seed=seed)
         block.join_forward(x, s["f"], s["y"], None, w_post=p["w_post"], gate=p["gate"], seed=seed)
-        off = s["y"].float() - target.float()
-        block.join_backward(None, off.to(x.dtype), None, s["f"], None, s["df"], w_post=p["w_post"], gate=p["gate"],
+        if self.teacher:
+            loss, dy = self._distance(block, s, x), s["dy"]
+        else:
+            off = s["y"].float() - target.float()
+            loss, dy = off.square().mean() / 2, off.to(x.dtype)
+        block.join_backward(None, dy, None, s["f"], None, s["df"], w_post=p["w_post"], gate=p["gate"],
                             dw_post=grad["w_post"], dgate=grad["gate"], seed=seed)
         block.ffn_backward(s["n"], p["W_in"], p["W_out"], s["saved"], s["df"], s["dn"], grad["W_in"], grad["W_out"])
         s["first"].join_backward(s["dn"], None, x, None, None, None, w_pre=p["w_pre"], dw_pre=grad["w_pre"])
-        return off.square().mean() / 2
+        return loss
 
     def step(self, number, rate=0.5):
         """One training step; returns its loss (a tensor on the device)."""
@@ -116,8 +150,9 @@ def main(argv=None):
     ap.add_argument("--mode", choices=sorted(TORCH), default="bf16")
     ap.add_argument("--dropout", type=float, default=0.1)
     ap.add_argument("--rate", type=float, default=0.5)
+    ap.add_argument("--teacher", type=int, default=0, metavar="K", help="learn from a teacher's K largest logits")
     a = ap.parse_args(argv)
-    t = Trainer(a.nodes, a.replication, a.width, a.hidden, a.tokens, a.mode, a.dropout)
+    t = Trainer(a.nodes, a.replication, a.width, a.hidden, a.tokens, a.mode, a.dropout, teacher=a.teacher)
     print(f"{a.nodes} nodes, {len(t.tokens)} files on {a.replication} of them each, {t.x.shape[0]} tokens, "
           f"{t.plan.Q * t.plan.T} parameters a row, {a.mode}")
     for number in range(a.steps):

@@ -123,6 +123,25 @@ def test_product(blocks, mode, rows, wide, outputs, pad):
 
 
 @pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("rows", [1, 4, 5, 8, 9, 16, 17, 32, 33, 64])
+@pytest.mark.parametrize("wide,outputs", [(1024, 50), (1152, 2047), (1664, 2050), (2176, 8195)])
+def test_product_of_few_rows(blocks, mode, rows, wide, outputs):
+    """The kernels that take the weights from memory to the matrix instructions, with parts of k that end before others, groups of rows
+    past the last, and more workgroups of two groups; all columns of some rows of the weights where these are many."""
+    x, xs = random_packed(rows + wide, rows, wide)
+    w, ws = random_packed(outputs, outputs, wide)
+    ws[:, wide // 128:] = 255                     # bytes past the last block say nothing
+    y, room = guarded(rows, outputs, R.DTYPES[mode], 1)
+    blocks[mode].packed_product(x, xs, w, ws, y)
+    torch.cuda.synchronize()
+    assert untouched(room, y)
+    picked = torch.unique(torch.cat((torch.arange(0, outputs, 1 + outputs // 60), torch.arange(max(0, outputs - 20), outputs))))
+    want, off = R.product(R.values(x, xs), R.values(w[picked.cuda()], ws[picked.cuda()]), mode)
+    got = y.double().cpu()[:, picked]
+    assert bool(((got - want).abs() <= off).all()), float(((got - want).abs() / off).max())
+
+
+@pytest.mark.parametrize("mode", MODES)
 @pytest.mark.parametrize("rows,wide,outputs", [(2049, 128, 4100), (4096, 256, 2304), (1030, 384, 5003), (700, 2304, 900)])
 def test_products_of_many_tiles(blocks, mode, rows, wide, outputs):
     """Tiles of both sizes, with edges; compared where the definition is affordable: some rows, some columns."""
@@ -140,15 +159,15 @@ def test_products_of_many_tiles(blocks, mode, rows, wide, outputs):
 
 
 @pytest.mark.parametrize("mode", MODES)
-@pytest.mark.parametrize("rows", [1, 20, 100])
-def test_product_of_what_is_no_number(blocks, mode, rows):
+@pytest.mark.parametrize("rows,wide", [(1, 512), (20, 512), (100, 512), (1, 1152), (7, 1152), (16, 1664), (30, 1152), (60, 1664)])
+def test_product_of_what_is_no_number(blocks, mode, rows, wide):
     """A NaN, and a block that is none, reach their own row or column and no other; zeros against them are none either."""
-    x, xs = random_packed(1, rows, 512)
-    w, ws = random_packed(2, 40, 512)
+    x, xs = random_packed(1, rows, wide)
+    w, ws = random_packed(2, 40, wide)
     x[rows - 1, 300] = 0x7F
     w[3, 17] = 0xFF
     ws[7, 2] = 255
-    ws[:, 4:] = 255                               # bytes past the last block say nothing
+    ws[:, wide // 128:] = 255                     # bytes past the last block say nothing
     y = torch.zeros(rows, 40, dtype=R.DTYPES[mode], device="cuda")
     blocks[mode].packed_product(x, xs, w, ws, y)
     want = torch.zeros(rows, 40, dtype=torch.bool)
@@ -554,3 +573,17 @@ def test_largest_rows(blocks):
                  lambda: block.distill(z, one(torch.int32), one(torch.float32), one(torch.float32)[0], None)):
         with pytest.raises(L.CcdcError):
             call()
+
+
+@pytest.mark.parametrize("mode", MODES)
+def test_products_of_more_than_64_rows_are_the_same_in_any_batch(blocks, mode):
+    """An element's sum has one order whatever tile it is in: nodes that have some of the rows make the same bits of them."""
+    wide, outputs = 1152, 2100
+    x, xs = random_packed(1, 3000, wide)
+    w, ws = random_packed(2, outputs, wide)
+    whole = torch.zeros(3000, outputs, dtype=R.DTYPES[mode], device="cuda")
+    blocks[mode].packed_product(x, xs, w, ws, whole)
+    for rows, columns in ((65, outputs), (333, outputs), (1000, outputs), (500, 70), (2999, 1)):
+        y = torch.zeros(rows, columns, dtype=R.DTYPES[mode], device="cuda")
+        blocks[mode].packed_product(x[:rows], xs[:rows], w[:columns], ws[:columns], y)
+        assert torch.equal(y, whole[:rows, :columns]), (rows, columns)
