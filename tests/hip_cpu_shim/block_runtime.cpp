@@ -40,6 +40,7 @@ enum class At { ready, wave, block, done };
 struct Copy {
     unsigned char *to;
     const void *from;
+    int bytes;
 };
 struct Lane {
     ucontext_t ctx;
@@ -205,12 +206,14 @@ uint32_t read_lane(uint32_t v, int lane)
 
 uint32_t update_dpp(uint32_t old, uint32_t v, int control, int rows, int banks, bool bound)
 {
-    if (banks != 15 || !bound) std::abort();
+    if (banks != 15) std::abort();
     give(&v, 4);
     const int lane = running % kWave;
-    uint32_t got = 0;
+    uint32_t got = bound ? 0 : old;                   // where nothing comes from
     if (control > 0x110 && control < 0x120) {         // shifted up within sixteen lanes
         if (lane % 16 >= control - 0x110) std::memcpy(&got, of_lane(lane - (control - 0x110)), 4);
+    } else if (control > 0x120 && control < 0x130) {  // rotated within sixteen lanes
+        std::memcpy(&got, of_lane(lane / 16 * 16 + (lane + 16 - (control - 0x120)) % 16), 4);
     } else if (control == 0x142) {                    // the last of each sixteen to the next
         if (lane >= 16) std::memcpy(&got, of_lane(lane / 16 * 16 - 1), 4);
     } else if (control == 0x143) {                    // lane 31 to the upper half
@@ -221,14 +224,81 @@ uint32_t update_dpp(uint32_t old, uint32_t v, int control, int rows, int banks, 
     return rows >> (lane / 16) & 1 ? got : old;
 }
 
+uint64_t ballot(bool v)
+{
+    const unsigned char mine = v;
+    give(&mine, 1);
+    uint64_t all = 0;
+    for (int l = 0; l < kWave; l++) all |= (uint64_t)(*of_lane(l) & 1) << l;
+    return all;
+}
+
+float of_eight(unsigned char b)
+{
+    const int e = b >> 3 & 15, m = b & 7;
+    const float v = (b & 127) == 127 ? NAN : e ? std::ldexp(8.0f + m, e - 10) : std::ldexp((float)m, -9);
+    return b & 128 ? -v : v;
+}
+
+// a lane has 32 numbers of its row of either side and the row's scale; rows of the result as multiply_any
+template <int SIZE, int RESULTS>
+static void multiply_eight(const void *a, int scale_a, const void *b, int scale_b, float *c)
+{
+    unsigned char mine[64];
+    std::memcpy(mine, a, 32);
+    // (both sides are 66 bytes: one after the other)
+    unsigned char left[kWave][32], left_scale[kWave];
+    give(mine, 32);
+    for (int l = 0; l < kWave; l++) std::memcpy(left[l], of_lane(l), 32);
+    mine[0] = (unsigned char)scale_a;
+    give(mine, 1);
+    for (int l = 0; l < kWave; l++) left_scale[l] = *of_lane(l);
+    unsigned char right[kWave][32], right_scale[kWave];
+    give(b, 32);
+    for (int l = 0; l < kWave; l++) std::memcpy(right[l], of_lane(l), 32);
+    mine[0] = (unsigned char)scale_b;
+    give(mine, 1);
+    for (int l = 0; l < kWave; l++) right_scale[l] = *of_lane(l);
+    const auto power = [](int s) { return s == 255 ? NAN : std::ldexp(1.0, s - 127); };
+    const int lane = running % kWave, column = lane % SIZE, group = lane / SIZE;
+    for (int i = 0; i < RESULTS; i++) {
+        const int row = SIZE == 16 ? 4 * group + i : 8 * (i / 4) + 4 * group + i % 4;
+        double sum = c[i];
+        for (int g = 0; g < kWave / SIZE; g++) {
+            const int l = row + g * SIZE, r = column + g * SIZE;
+            double part = 0;
+            for (int e = 0; e < 32; e++) part += (double)of_eight(left[l][e]) * of_eight(right[r][e]);
+            sum += part * power(left_scale[l]) * power(right_scale[r]);
+        }
+        c[i] = (float)sum;
+    }
+}
+void multiply_eight16(const void *a, int sa, const void *b, int sb, float *c) { multiply_eight<16, 4>(a, sa, b, sb, c); }
+void multiply_eight32(const void *a, int sa, const void *b, int sb, float *c) { multiply_eight<32, 16>(a, sa, b, sb, c); }
+
+int to_eight(float v)
+{
+    if (!(std::fabs(v) < 464.5f)) return std::signbit(v) ? 0xFF : 0x7F;
+    int best = 0;
+    for (int b = 0; b < 127; b++) {                   // ties to the even one
+        const float off = std::fabs(of_eight((unsigned char)b) - std::fabs(v)), least = std::fabs(of_eight((unsigned char)best) - std::fabs(v));
+        if (off < least || (off == least && b % 2 == 0)) best = b;
+    }
+    return best | (std::signbit(v) ? 128 : 0);
+}
+
 void copy_to_lds(uint32_t to, const void *from)
 {
-    lanes[running].copies.push_back({lds + to + running % kWave * 16, from});
+    lanes[running].copies.push_back({lds + to + running % kWave * 16, from, 16});
+}
+void copy_words_to_lds(uint32_t to, const void *from)
+{
+    lanes[running].copies.push_back({lds + to + running % kWave * 4, from, 4});
 }
 
 __attribute__((optnone)) static void arrive(const Copy &c)       // byte by byte, each of them checked
 {
-    for (int i = 0; i < 16; i++) c.to[i] = static_cast<const unsigned char *>(c.from)[i];
+    for (int i = 0; i < c.bytes; i++) c.to[i] = static_cast<const unsigned char *>(c.from)[i];
 }
 
 void wait_copies(int but)
@@ -258,7 +328,7 @@ void multiply32(const uint16_t *a, const uint16_t *b, bool bf, float *c) { multi
 void launch(dim3 grid, dim3 block, size_t bytes, const std::function<void()> &kernel)
 {
     launches++;
-    if (!grid.x || !grid.y || !grid.z || grid.y > 65535 || grid.z > 65535 || !block.x || block.x > 1024 || block.y != 1 || block.z != 1 || bytes ||
+    if (!grid.x || !grid.y || !grid.z || grid.y > 65535 || grid.z > 65535 || !block.x || block.x > 1024 || block.y != 1 || block.z != 1 || bytes > max_dynamic_lds ||
         (uint64_t)grid.x * block.x >> 32) {
         std::fprintf(stderr, "shim: launch refused (grid %u %u %u, block %u)\n", grid.x, grid.y, grid.z, block.x);
         last_error = hipErrorInvalidValue;
@@ -278,7 +348,12 @@ void launch(dim3 grid, dim3 block, size_t bytes, const std::function<void()> &ke
         for (unsigned y = 0; y < grid.y; y++)
             for (unsigned x = 0; x < grid.x; x++) {
                 blockIdx = {x, y, z};
+                if (bytes) {
+                    dyn_smem = static_cast<unsigned char *>(std::malloc(bytes));
+                    std::memset(dyn_smem, 0xFF, bytes);
+                }
                 run_workgroup();
+                if (bytes) std::free(dyn_smem);
             }
 }
 }  // namespace shim

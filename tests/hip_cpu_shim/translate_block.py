@@ -23,8 +23,29 @@ def _shared(m):
     return f"auto &{name} = *static_cast<{kind} (*){dims}>(shim::block_shared(sizeof({kind}{dims}), {align}));"
 
 
+_COPIES = [
+    (r"#define CCDC_LDS .*", "#define CCDC_LDS", 1),
+    (r"const uint32_t lds_at = \(uint32_t\)\(uintptr_t\)lds;", "const uint32_t lds_at = 0; shim::lds = memory;", 1),
+    (r'asm volatile\("s_mov_b32 m0, %0[^;]*?dwordx4 %1, %2"[^;]*?"s"\(base\) : "memory"\);', "shim::copy_to_lds(to, (const char *)base + offset);", 1),
+    (r'asm volatile\("s_mov_b32 m0, %0[^;]*?dword %1, %2"[^;]*?"s"\(base\) : "memory"\);', "shim::copy_words_to_lds(to, (const char *)base + offset);", 1),
+    (r'asm volatile\("s_barrier" ::: "memory"\);', "shim::barrier_wait();", 1),
+    (r'asm volatile\("s_waitcnt vmcnt\(%0\) lgkmcnt\(0\)" ::"n"\((.*?)\) : "memory"\);', r"shim::wait_copies(\1);", 4),
+    (r'asm volatile\("s_waitcnt vmcnt\(0\) lgkmcnt\(0\)" ::: "memory"\);', "shim::wait_copies(0);", 2),
+    (r'asm volatile\("s_waitcnt lgkmcnt\(0\)" ::: "memory"\);', "", 1),
+]
+
 # file: (pattern, replacement, how often at least)
 RULES = {
+    "vocabulary.hpp": [(r'asm volatile\("" : "\+v"\([\w\[\]]+\)\);', ";", 2)],
+    "distill.hip": [(r"extern __shared__ uint32_t mask\[\];", "uint32_t *mask = reinterpret_cast<uint32_t *>(shim::dyn_smem);", 1)],
+    "eight.hip": [(r"return few_rows8\(b, a\) \?", "return shim::force < 0 && few_rows8(b, a) ?", 1)],
+    "product8.hip": _COPIES + [
+        (r"(?=\n#pragma unroll\n        for \(int q = 0; q < 4; q\+\+\) \{\n            const uint32_t row = q \* 8)", "\n        shim::wave_in_step();", 1),
+        (r"if \(largest <= least\)", "if (shim::force >= 0 ? shim::force == 1 : largest <= least)", 1),
+        (r"if \(small == least\)", "if (shim::force >= 0 ? shim::force == 2 : small == least)", 1),
+        (r"if \(tall == least\)", "if (shim::force >= 0 ? shim::force == 3 : tall == least)", 1),
+        (r"if \(one == least\)", "if (shim::force >= 0 ? shim::force == 4 : one == least)", 1),
+    ],
     "element.hpp": [(r'asm volatile\("" : "\+[vs]"\(v\)\);', "", 2)],
     "join.hip": [(r"\(const __attribute__\(\(address_space\(4\)\)\) JoinArgs \*\)__builtin_amdgcn_kernarg_segment_ptr\(\)", "&a", 1)],
     "product.hip": [
@@ -50,6 +71,7 @@ def translate_block(text, name):
         if count < least:
             raise SystemExit(f"{name}: {pattern!r} found {count} times, not {least}")
     text = re.sub(r"__shared__\s+(?:__attribute__\(\(aligned\((\d+)\)\)\)\s+)?([\w ]+?)\s+(\w+)((?:\[[^\]]+\])+);", _shared, text)
+    text = re.sub(r"__shared__\s+(\w+)\s+(\w+);", r"auto &\2 = *static_cast<\1 *>(shim::block_shared(sizeof(\1), 16));", text)
     text = translate.translate(text)
     code = re.sub(r"#ifdef __HIP_DEVICE_COMPILE__.*?#(else|endif)", "", re.sub(r"//.*", "", text), flags=re.S)
     for left in ("__shared__", "<<<", "asm volatile", "address_space"):
