@@ -34,13 +34,13 @@ struct Listed {
 // Three terms' worth of rounding is all that exp(x) = 2^(x log2 e) adds in fp32 for what exp gives of |x| < 100.
 __device__ __forceinline__ float exponential(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
-template <class T, int WAVES, int PACKS>
-__global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
+template <class T, int WAVES, int PACKS, int LDS, bool REST>
+__global__ __launch_bounds__(64 * WAVES, LDS > 0 ? 8 : 0) void k_distill(const DistillArgs a)
 {
     using E = typename T::elem;
     constexpr int THREADS = 64 * WAVES;
-    constexpr bool kept = PACKS > 0 && T::planes == 3;        // fp32: the exponentials take the logits' registers
-    extern __shared__ uint32_t mask[];            // a bit a column, lowest first
+    constexpr bool kept = !REST && T::planes == 3;        // fp32: the exponentials take the logits' registers
+    extern __shared__ __attribute__((aligned(16))) uint32_t mask[];       // a bit a column, lowest first; then packs of the row
     __shared__ double part[2 * WAVES];
     __shared__ int32_t listed[kMostListed];
     __shared__ Listed shared;
@@ -50,7 +50,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
     const bool lists = threadIdx.x < 64;          // the list's wavefront
     const float factor = a.weight ? a.weight[row] * a.scale : a.scale;
     const bool counts = !(a.weight && a.weight[row] == 0.0f);
-    Row<T, WAVES, PACKS> z;
+    Row<T, WAVES, PACKS, LDS, REST> z;
+    z.room = reinterpret_cast<Bytes16 *>(mask + a.mask_bytes / 4) + threadIdx.x;
     if (counts) z.load(a.z, row * a.ldz, a.columns);
     for (int i = threadIdx.x; i < a.mask_bytes / 4; i += THREADS) mask[i] = 0;
 
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
     const auto listed_of = [&](int32_t c) { return (uint32_t)((((uint64_t)mask[c / 32 + 1] << 32) | mask[c / 32]) >> (c % 32)) & 0xFFu; };
     const float scale = a.per_T * kLog2e;
     float m = -INFINITY, s = 0.0f;
-    if constexpr (PACKS > 0) {
+    if constexpr (!REST) {
         z.template hide_held<false>(listed_of, [&](const Eight &v) {
 #pragma unroll
             for (int i = 0; i < 8; i++) m = fmaxf(m, v.v[i]);
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
     } else {
         // the largest so far and the sum from it on
         float from = kLowest;
-        z.each(listed_of, [&](const Eight &v, int32_t, uint32_t) {
+        const auto arrives = [&](const Eight &v) {
             float next = m;
 #pragma unroll
             for (int i = 0; i < 8; i++) next = fmaxf(next, v.v[i]);
@@ -137,21 +138,27 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
             }
 #pragma unroll
             for (int i = 0; i < 8; i++) s += __builtin_amdgcn_exp2f((v.v[i] - from) * scale);
-        });
+        };
+        z.template hide_held<false>(listed_of, arrives);
+        z.rest(listed_of, [&](const Eight &v, int32_t, uint32_t) { arrives(v); });
         const float own = m;
         m = over.most(m);
         s = over.sum(s * __builtin_amdgcn_exp2f((own - fmaxf(m, kLowest)) * scale));
     }
-    Powers powers(scale, fmaxf(m, kLowest));
-    if constexpr (PACKS > 0) {
-        if (powers.far()) {                       // (the same for all threads)
-            z.subtract(powers.from);
-            powers = Powers(scale, 0.0f);
-        }
-        z.whole();
+    const Powers powers(scale, fmaxf(m, kLowest));
+    const bool far = REST || kept || powers.far();        // (the same for all threads)
+    if constexpr (!REST) {
         PackSum sum;
         const auto add = [&](const Eight &e) {
             sum.add(((e.v[0] + e.v[1]) + (e.v[2] + e.v[3])) + ((e.v[4] + e.v[5]) + (e.v[6] + e.v[7])));
+        };
+        const auto sums = [&](auto &row, auto term) {
+            row.each(listed_of, [&](const Eight &v, int32_t, uint32_t) {
+                Eight e;
+#pragma unroll
+                for (int i = 0; i < 8; i++) e.v[i] = term(v.v[i]);
+                add(e);
+            });
         };
         if constexpr (kept) {
 #pragma unroll
@@ -160,20 +167,18 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
                 Eight e;
 #pragma unroll
                 for (int k = 0; k < 8; k++) {
-                    e.v[k] = powers(__uint_as_float(z.held[i][k]));
+                    e.v[k] = powers.difference(__uint_as_float(z.held[i][k]));
                     z.held[i][k] = __float_as_uint(e.v[k]);
                 }
                 add(e);
             }
+        } else if (far) {                         // few rows: read again
+            auto again = z.again();
+            sums(again, [&](float v) { return powers.difference(v); });
         } else {
-            z.each(listed_of, [&](const Eight &v, int32_t, uint32_t) {
-                Eight e;
-#pragma unroll
-                for (int i = 0; i < 8; i++) e.v[i] = powers(v.v[i]);
-                add(e);
-            });
+            sums(z, [&](float v) { return powers(v); });
         }
-        s = over.sum(sum) * powers.lost();
+        s = over.sum(sum) * (far ? 1.0f : powers.lost());
     }
 
     // all relative to the row's largest logit
@@ -204,15 +209,27 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
     }
     if (!a.dz) return;
     const float of_rest = list.p_rest == 0.0f || s == 0.0f ? 0.0f : list.p_rest / s;
-    const float C = factor * a.per_T * (others_exp / total - of_rest) * (PACKS > 0 ? powers.lost() : 1.0f);
+    const float C = factor * a.per_T * (others_exp / total - of_rest) * (far ? 1.0f : powers.lost());
     E *dz = (E *)a.dz + row * a.lddz;
-    z.each(listed_of, [&](const Eight &v, int32_t c, uint32_t valid) {
-        if (PACKS > 0 && !valid) return;
-        Eight d;
+    const auto made = [&](auto &row, auto term) {
+        row.each(listed_of, [&](const Eight &v, int32_t c, uint32_t valid) {
+            if (!valid) return;
+            Eight d;
 #pragma unroll
-        for (int i = 0; i < 8; i++) d.v[i] = C * (kept ? v.v[i] : PACKS > 0 ? powers(v.v[i]) : powers.difference(v.v[i]));
-        z.store(dz + c, d, valid);
-    });
+            for (int i = 0; i < 8; i++) d.v[i] = C * term(v.v[i]);
+            row.store(dz + c, d, valid);
+        });
+    };
+    if constexpr (REST) {
+        made(z, [&](float v) { return powers.difference(v); });
+    } else if constexpr (kept) {
+        made(z, [](float v) { return v; });
+    } else if (far) {
+        auto again = z.again();
+        made(again, [&](float v) { return powers.difference(v); });
+    } else {
+        made(z, [&](float v) { return powers(v); });
+    }
     __syncthreads();                              // the list's columns are written over
     if (lists)
 #pragma unroll
@@ -220,34 +237,40 @@ __global__ __launch_bounds__(64 * WAVES) void k_distill(const DistillArgs a)
             if (column[h] >= 0) dz[column[h]] = narrow<T>(gradient[h]);
 }
 
-// Wavefronts of a row and packs that a lane holds of it: launch(waves, packs), packs 0 where the row is more than the registers hold.
+// launch(wavefronts of a row, packs that a lane holds of it in registers, in LDS, whether the row may be longer).
 template <class T, class F>
 int by_columns(int64_t columns, int64_t rows, F launch)
 {
-    using std::integral_constant;
+    const auto go = [&](auto waves, auto packs) { return launch(waves, packs, std::integral_constant<int, 0>(), std::false_type()); };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 4> four;
+    const std::integral_constant<int, 8> eight;
+    const std::integral_constant<int, 16> sixteen;
     const int64_t packs = (columns + 7) / 8;
-#ifdef VW
-    return launch(integral_constant<int, VW>(), integral_constant<int, VP>());
-#endif
     const bool few = rows <= 256;
-    if (packs <= 64) return launch(integral_constant<int, 1>(), integral_constant<int, 1>());
-    if (packs <= 128) return launch(integral_constant<int, 1>(), integral_constant<int, 2>());
-    if (packs <= 256 && !few) return launch(integral_constant<int, 2>(), integral_constant<int, 2>());
-    if (packs <= 512) return few ? launch(integral_constant<int, 4>(), integral_constant<int, 2>()) : launch(integral_constant<int, 2>(), integral_constant<int, 4>());
-    if (packs <= 1024) return launch(integral_constant<int, 4>(), integral_constant<int, 4>());
-    if (packs <= 2048) return launch(integral_constant<int, 8>(), integral_constant<int, 4>());
-    if (packs <= 4096) return few ? launch(integral_constant<int, 16>(), integral_constant<int, 4>()) : launch(integral_constant<int, 8>(), integral_constant<int, 8>());
-    if (packs <= 8192 && T::planes == 3) return launch(integral_constant<int, 16>(), integral_constant<int, 8>());
-    return launch(integral_constant<int, 16>(), integral_constant<int, 0>());
+    if (packs <= 64) return go(one, one);
+    if (packs <= 128) return go(one, two);
+    if (packs <= 256 && !few) return go(two, two);
+    if (packs <= 512) return few ? go(four, two) : go(two, four);
+    if (packs <= 1024) return go(four, four);
+    if (packs <= 2048) return go(eight, four);
+    if (packs <= 4096) return few ? go(sixteen, four) : go(eight, eight);
+    if constexpr (T::planes == 1) {
+        if (packs <= 8192) return launch(sixteen, four, four, std::false_type());
+        return launch(sixteen, four, std::integral_constant<int, 3>(), std::true_type());
+    }
+    if (packs <= 8192) return go(sixteen, eight);
+    return launch(sixteen, std::integral_constant<int, 0>(), std::integral_constant<int, 0>(), std::true_type());
 }
 
 template <class T>
 int run_distill(const DistillArgs &a, int64_t rows, hipStream_t st)
 {
-    return by_columns<T>(a.columns, rows, [&](auto waves, auto packs) -> int {
-        constexpr int W = decltype(waves)::value, P = decltype(packs)::value;
+    return by_columns<T>(a.columns, rows, [&](auto waves, auto packs, auto lds, auto rest) -> int {
+        constexpr int W = decltype(waves)::value, P = decltype(packs)::value, L = decltype(lds)::value;
         if (!fits_launch((uint64_t)rows * 64 * W)) return CCDC_ESIZE;
-        k_distill<T, W, P><<<(uint32_t)rows, 64 * W, a.mask_bytes, st>>>(a);
+        k_distill<T, W, P, L, decltype(rest)::value><<<(uint32_t)rows, 64 * W, a.mask_bytes + L * 64 * W * 16, st>>>(a);
         return launched();
     });
 }
@@ -271,7 +294,7 @@ int ccdc_distill(const ccdc_block_t *b, int64_t rows, int64_t columns, const voi
     for (const void *p : {(const void *)index, (const void *)value, (const void *)rest, (const void *)weight, (const void *)loss})
         if (!aligned(p, 4)) return CCDC_EINVAL;
     if (columns > kMostColumns) return CCDC_ESIZE;
-    const DistillArgs a{z, index, value, rest, weight, loss, dz, ldz, lddz, (int32_t)columns, k, (int32_t)((columns / 32 + 2) * 4), per_T,
+    const DistillArgs a{z, index, value, rest, weight, loss, dz, ldz, lddz, (int32_t)columns, k, (int32_t)((columns / 32 + 2 + 3) / 4 * 16), per_T,
                         (float)scale};
     CCDC_BY_ELEM(b, (run_distill<T>(a, rows, (hipStream_t)stream)));
 }

@@ -120,16 +120,36 @@ __device__ __forceinline__ uint32_t hide_word(uint32_t word, uint32_t bits, int 
 
 // A row in packs of eight columns.  The last is read as the row's last eight, and what the one before has too is hidden: every read
 // is of eight columns in the row, also those of lanes past its end, and none takes a way of its own.
-// A thread has packs (its place) + i * (threads).  PACKS > 0: as many at the most, held in registers as loaded; 0: any number, read
-// whenever they are asked for.  What is hidden is -infinity.
-template <class T, int WAVES, int PACKS>
+// A thread has packs (its place) + i * (threads): the first PACKS held in registers as loaded, LDS more in LDS, and, where the row is longer
+// (REST), any number that are read whenever they are asked for.  What is hidden is -infinity.
+template <class T, int WAVES, int PACKS, int LDS = 0, bool REST = PACKS == 0>
 struct Row {
     using E = typename T::elem;
-    static constexpr int kThreads = 64 * WAVES, kWords = 2 * sizeof(E);
+    static constexpr int kThreads = 64 * WAVES, kWords = 2 * sizeof(E), HELD = PACKS + LDS;
+    static_assert(LDS == 0 || kWords == 4);
     const E *p;
     int32_t columns;
     uint32_t held[PACKS ? PACKS : 1][kWords];
+    Bytes16 *room;                        // the thread's first pack in LDS
 
+    __device__ __forceinline__ void get(int i, uint32_t (&words)[kWords]) const
+    {
+        if (i < PACKS) {
+#pragma unroll
+            for (int w = 0; w < kWords; w++) words[w] = held[i < PACKS ? i : 0][w];
+        } else {
+            __builtin_memcpy(words, &room[(i - PACKS) * kThreads], 16);
+        }
+    }
+    __device__ __forceinline__ void set(int i, const uint32_t (&words)[kWords])
+    {
+        if (i < PACKS) {
+#pragma unroll
+            for (int w = 0; w < kWords; w++) held[i < PACKS ? i : 0][w] = words[w];
+        } else {
+            __builtin_memcpy(&room[(i - PACKS) * kThreads], words, 16);
+        }
+    }
     struct Pack8 {
         int32_t start;                    // first column that is read
         uint32_t valid;                   // of the eight: those that are this pack's
@@ -170,6 +190,15 @@ struct Row {
 #pragma unroll
         for (int i = 0; i < PACKS; i++)
             if (some(i)) read(held[i], pack_of(fresh((int32_t)threadIdx.x + i * kThreads)).start);
+        if constexpr (LDS > 0) {
+            uint32_t words[LDS][kWords];
+#pragma unroll
+            for (int i = 0; i < LDS; i++)
+                if (some(PACKS + i)) read(words[i], pack_of(fresh((int32_t)threadIdx.x + (PACKS + i) * kThreads)).start);
+#pragma unroll
+            for (int i = 0; i < LDS; i++)
+                if (some(PACKS + i)) set(PACKS + i, words[i]);
+        }
     }
     // Eight numbers, widened.  The compiler does not see that a held pack is what it was in another pass, or it would keep all 16-bit
     // numbers widened.
@@ -208,64 +237,65 @@ struct Row {
         const uint32_t shift = fresh_uniform(16u), mask = fresh_uniform(0xFFFF0000u);
         whole();
 #pragma unroll
-        for (int i = 0; i < PACKS; i++) {
+        for (int i = 0; i < HELD; i++) {
             if (!some(i)) continue;
             const Pack8 pack = pack_of(fresh((int32_t)threadIdx.x + i * kThreads));
             const uint32_t bits = (hidden(pack.start) | ~pack.valid) & 0xFFu;
-            if (!FEW || bits)
+            if (FEW && !bits) continue;
+            uint32_t words[kWords];
+            get(i, words);
 #pragma unroll
-                for (int w = 0; w < kWords; w++) held[i][w] = hide_word<T>(held[i][w], bits, w);
-            if constexpr (!FEW) f(wide(held[i], shift, mask));
+            for (int w = 0; w < kWords; w++) words[w] = hide_word<T>(words[w], bits, w);
+            set(i, words);
+            if constexpr (!FEW) f(wide(words, shift, mask));
         }
         whole();
         if constexpr (FEW)
 #pragma unroll
-            for (int i = 0; i < PACKS; i++)
-                if (some(i)) f(wide(held[i], shift, mask));
-    }
-    // All numbers less what they have in common.  Exact where it matters: of rows so far from zero (Powers) the differences that are no
-    // whole few steps of the type are exponentials of zero.
-    __device__ __forceinline__ void subtract(float from)
-    {
-#pragma unroll
-        for (int i = 0; i < PACKS; i++) {
-            Raw8<T> raw;
-            __builtin_memcpy(&raw, held[i], sizeof raw);
-#pragma unroll
-            for (int e = 0; e < 8; e++) raw.p.v[e] = narrow<T>(T::widen(raw.p.v[e]) - from);
-            __builtin_memcpy(held[i], &raw, sizeof raw);
-        }
+            for (int i = 0; i < HELD; i++) {
+                if (!some(i)) continue;
+                uint32_t words[kWords];
+                get(i, words);
+                f(wide(words, shift, mask));
+            }
     }
     // f(values, first of their eight columns, which of them are this pack's) for each pack; those that are read now are hidden now.
     template <class H, class F>
     __device__ __forceinline__ void each(H hidden, F f)
     {
         const uint32_t shift = fresh_uniform(16u), mask = fresh_uniform(0xFFFF0000u);
-        if constexpr (PACKS > 0) {
 #pragma unroll
-            for (int i = 0; i < PACKS; i++) {
-                if (!some(i)) continue;
-                const Pack8 pack = pack_of(fresh((int32_t)threadIdx.x + i * kThreads));
-                f(wide(held[i], shift, mask), pack.start, pack.valid);
-                // one after the other: with packs interleaved a row of eight takes half as many registers again
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-            // two packs on their way at a time
-            const int32_t packs = (columns + 7) / 8;
-            for (int32_t j = (int32_t)threadIdx.x; j < packs; j += 2 * kThreads) {
-                const Pack8 pack[2] = {pack_of(j), pack_of(j + kThreads)};
-                uint32_t words[2][kWords];
+        for (int i = 0; i < HELD; i++) {
+            if (!some(i)) continue;
+            const Pack8 pack = pack_of(fresh((int32_t)threadIdx.x + i * kThreads));
+            uint32_t words[kWords];
+            get(i, words);
+            f(wide(words, shift, mask), pack.start, pack.valid);
+            // one after the other: with packs interleaved a row of eight takes half as many registers again
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        rest(hidden, f);
+    }
+    // Of those that are not held.
+    template <class H, class F>
+    __device__ __forceinline__ void rest(H hidden, F f)
+    {
+        if constexpr (!REST) return;
+        const uint32_t shift = fresh_uniform(16u), mask = fresh_uniform(0xFFFF0000u);
+        // two packs on their way at a time
+        const int32_t packs = (columns + 7) / 8;
+        for (int32_t j = (int32_t)threadIdx.x + HELD * kThreads; j < packs; j += 2 * kThreads) {
+            const Pack8 pack[2] = {pack_of(j), pack_of(j + kThreads)};
+            uint32_t words[2][kWords];
 #pragma unroll
-                for (int h = 0; h < 2; h++) read(words[h], pack[h].start);
+            for (int h = 0; h < 2; h++) read(words[h], pack[h].start);
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const uint32_t bits = (hidden(pack[h].start) | ~pack[h].valid) & 0xFFu;
-                    if (bits)             // few packs
+            for (int h = 0; h < 2; h++) {
+                const uint32_t bits = (hidden(pack[h].start) | ~pack[h].valid) & 0xFFu;
+                if (bits)                 // few packs
 #pragma unroll
-                        for (int w = 0; w < kWords; w++) words[h][w] = hide_word<T>(words[h][w], bits, w);
-                    if (pack[h].valid) f(wide(words[h], shift, mask), pack[h].start, pack[h].valid);
-                }
+                    for (int w = 0; w < kWords; w++) words[h][w] = hide_word<T>(words[h][w], bits, w);
+                if (pack[h].valid) f(wide(words[h], shift, mask), pack[h].start, pack[h].valid);
             }
         }
     }
@@ -273,7 +303,7 @@ struct Row {
     // what is read (1500 x 131071 f16 250 -> 233 us).
     static __device__ __forceinline__ void store(E *to, const Eight &v, uint32_t valid)
     {
-        if (valid == 0xFFu && PACKS == 0) {
+        if (valid == 0xFFu && REST) {
             constexpr int W = 16 / sizeof(E);
             using P = Pack<E, W>;
 #pragma unroll

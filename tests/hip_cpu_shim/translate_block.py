@@ -37,7 +37,7 @@ _COPIES = [
 # file: (pattern, replacement, how often at least)
 RULES = {
     "vocabulary.hpp": [(r'asm volatile\("" : "\+v"\([\w\[\]]+\)\);', ";", 2)],
-    "distill.hip": [(r"extern __shared__ uint32_t mask\[\];", "uint32_t *mask = reinterpret_cast<uint32_t *>(shim::dyn_smem);", 1)],
+    "distill.hip": [(r"extern __shared__ __attribute__\(\(aligned\(16\)\)\) uint32_t mask\[\];", "uint32_t *mask = reinterpret_cast<uint32_t *>(shim::dyn_smem);", 1)],
     "eight.hip": [(r"return few_rows8\(b, a\) \?", "return shim::force < 0 && few_rows8(b, a) ?", 1)],
     "product8.hip": _COPIES + [
         (r"(?=\n#pragma unroll\n        for \(int q = 0; q < 4; q\+\+\) \{\n            const uint32_t row = q \* 8)", "\n        shim::wave_in_step();", 1),
