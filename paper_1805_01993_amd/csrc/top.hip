@@ -195,7 +195,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
         return over.sum(sum);
     };
     if (kth && !powers.far()) {
-        sum = sum_of(z, [&](float v, int32_t) { return powers(v > least ? least : v); });
+        // (a NaN is the smaller of two numbers here: one instruction, where a comparison and a choice are two)
+        const float one = fmaf(least, scale, -powers.K);
+        sum = sum_of(z, [&](float v, int32_t) { return __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(fmaf(v, scale, -powers.K), one)); });
         const float listed = (float)a.k * powers(least);
         sum = sum - listed < listed ? 0.0f : (sum - listed) * powers.lost();
     }
