@@ -31,7 +31,7 @@ struct Listed {
     int count;                                    // entries; 0 too where they and the rest are all -infinity
 };
 
-// Three terms' worth of rounding is all that exp(x) = 2^(x log2 e) adds in fp32 for what exp gives of |x| < 100.
+// exp(x) = 2^(x log2 e): rounding the product is off by half a step of it, |x| 2^-24 of the result.
 __device__ __forceinline__ float exponential(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 template <class T, int WAVES, int PACKS, int LDS, bool REST>
@@ -237,6 +237,10 @@ __global__ __launch_bounds__(64 * WAVES, LDS > 0 ? 8 : 0) void k_distill(const D
             if (column[h] >= 0) dz[column[h]] = narrow<T>(gradient[h]);
 }
 
+// Of rows with more packs none is held: their bits and packs in LDS would leave a compute unit no second workgroup, and from 900000
+// columns on not one (16 bits, dz too: 600 x 300000 212 us held, 232 not; 300 x 600000 260 and 253).
+constexpr int64_t kMostHeld = 65536;
+
 // launch(wavefronts of a row, packs that a lane holds of it in registers, in LDS, whether the row may be longer).
 template <class T, class F>
 int by_columns(int64_t columns, int64_t rows, F launch)
@@ -258,7 +262,7 @@ int by_columns(int64_t columns, int64_t rows, F launch)
     if (packs <= 4096) return few ? go(sixteen, four) : go(eight, eight);
     if constexpr (T::planes == 1) {
         if (packs <= 8192) return launch(sixteen, four, four, std::false_type());
-        return launch(sixteen, four, std::integral_constant<int, 3>(), std::true_type());
+        if (packs <= kMostHeld) return launch(sixteen, four, std::integral_constant<int, 3>(), std::true_type());
     }
     if (packs <= 8192) return go(sixteen, eight);
     return launch(sixteen, std::integral_constant<int, 0>(), std::integral_constant<int, 0>(), std::true_type());

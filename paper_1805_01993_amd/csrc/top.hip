@@ -224,9 +224,6 @@ int by_columns(int64_t columns, int64_t rows, F launch)
 {
     using std::integral_constant;
     const int64_t packs = (columns + 7) / 8;
-#ifdef VW
-    return launch(integral_constant<int, VW>(), integral_constant<int, VP>());
-#endif
     const bool few = rows <= 256;
     if (packs <= 64) return launch(integral_constant<int, 1>(), integral_constant<int, 1>());
     if (packs <= 128) return launch(integral_constant<int, 1>(), integral_constant<int, 2>());

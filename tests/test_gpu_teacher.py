@@ -576,6 +576,15 @@ def test_largest_rows(blocks):
 
 
 @pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("columns", [524288, 524289, 1 << 20])
+def test_long_rows(blocks, mode, columns):
+    """Rows that are held in part, and those of which none is: more bits of listed columns than leave room for it."""
+    z = noise(7, 2, columns).to(R.DTYPES[mode]).cuda()
+    index = torch.tensor([[columns - 1, 0, 70001], [131071, 32768, columns - 2]])
+    check_distill(blocks[mode], mode, z, index, noise(8, 2, 3), noise(9, 2), 1.5)
+
+
+@pytest.mark.parametrize("mode", MODES)
 def test_products_of_more_than_64_rows_are_the_same_in_any_batch(blocks, mode):
     """An element's sum has one order whatever tile it is in: nodes that have some of the rows make the same bits of them."""
     wide, outputs = 1152, 2100
