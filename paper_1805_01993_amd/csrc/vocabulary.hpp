@@ -229,28 +229,27 @@ struct Row {
 #pragma unroll
             for (int w = 0; w < kWords; w++) asm volatile("" : "+v"(held[i][w]));
     }
-    // Hides the columns of held packs that hidden(first of eight columns) has bits of, and f(values) for each pack.  FEW: where only few packs
-    // have any, they alone do it (with many that is a way past half of them, and more registers).
-    template <bool FEW, class H, class F>
+    // Hides the columns of held packs that hidden(first of eight columns) has bits of, and f(values) for each pack.  END: only what is past the
+    // row's end is hidden, of the packs there.
+    template <bool END, class H, class F>
     __device__ __forceinline__ void hide_held(H hidden, F f)
     {
         const uint32_t shift = fresh_uniform(16u), mask = fresh_uniform(0xFFFF0000u);
         whole();
 #pragma unroll
         for (int i = 0; i < HELD; i++) {
-            if (!some(i)) continue;
+            if (!some(i) || (END && (i + 1) * kThreads * 8 <= columns)) continue;
             const Pack8 pack = pack_of(fresh((int32_t)threadIdx.x + i * kThreads));
             const uint32_t bits = (hidden(pack.start) | ~pack.valid) & 0xFFu;
-            if (FEW && !bits) continue;
             uint32_t words[kWords];
             get(i, words);
 #pragma unroll
             for (int w = 0; w < kWords; w++) words[w] = hide_word<T>(words[w], bits, w);
             set(i, words);
-            if constexpr (!FEW) f(wide(words, shift, mask));
+            if constexpr (!END) f(wide(words, shift, mask));
         }
         whole();
-        if constexpr (FEW)
+        if constexpr (END)
 #pragma unroll
             for (int i = 0; i < HELD; i++) {
                 if (!some(i)) continue;
