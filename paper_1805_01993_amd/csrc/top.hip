@@ -3,8 +3,10 @@
 // A workgroup has a row, held in registers where it fits.  The k-th largest of the threads' own largest values is a bound that at
 // least k values reach and few more: with each thread's value in LDS, sixteen bounds at a time are counted by ballots, so five rounds find
 // twenty bits of it.  What reaches it is put into a list in LDS, whatever the order, and ranked there: as keys of 64 bits, value then
-// column, no two are equal, so the order is one.  A row of which too much reaches the bound (many equal values) is counted again
-// bit by bit, values first and then columns, until exactly k are left.
+// column, no two are equal, so the order is one.  Where the list is long for its k (short rows of which much is wanted) the k-th
+// largest in it is found first, by ballots, bit by bit.  Where there is no room for all that reaches the bound (many equal values, those
+// of a mask by the lowest number among them) the row is counted again by digits of eight bits of those keys, values first and then
+// columns, until what is left has room.
 #include "vocabulary.hpp"
 
 namespace {
@@ -32,11 +34,13 @@ __device__ __forceinline__ float value_of(uint32_t key)
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
 
+constexpr int kFew = 96;                          // of the list: not worth a search of the k-th
+
 template <class T, int WAVES, int PACKS>
 __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
 {
     constexpr int THREADS = 64 * WAVES, DIGITS = 16 / WAVES, ROUNDS = std::is_same<T, ElemBF16>::value ? 4 : 5;
-    constexpr int kRoom = WAVES == 1 ? 256 : WAVES <= 4 ? 1024 : 2048;  // of the list
+    constexpr int kRoom = WAVES == 1 ? 512 : WAVES <= 4 ? 1024 : 2048;  // of the list
     __shared__ double part[2 * WAVES];
     __shared__ uint32_t largest[THREADS];
     __shared__ int32_t counts[2][16];
@@ -47,6 +51,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const auto none = [](int32_t) { return 0u; };
+    if (WAVES > 1 || PACKS > 1) __builtin_assume(a.columns >= 8);     // (by_columns; shorter rows' loads are many registers)
     Row<T, WAVES, PACKS> z;
     z.load(a.z, row * a.ldz, a.columns);
     float most = -INFINITY, pack_most[PACKS ? PACKS : 1] = {};
@@ -118,37 +123,89 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     __syncthreads();
     int32_t n = used;
     if (n > kRoom) {                              // (the same for all threads)
-        const auto count = [&](auto wanted) {
-            float sum = 0.0f;
+        // as numbers of 56 bits; the k-th's from the highest digit on, and `left` of what has the digits so far are wanted
+        const auto key_of = [](float v, int32_t c) { return (uint64_t)ordered(v) << 24 | (0xFFFFFFu - (uint32_t)c); };
+        int32_t *bins = reinterpret_cast<int32_t *>(found);
+        uint64_t key = 0;
+        int32_t left = a.k;
+        for (int shift = 48; shift >= 0 && n > kRoom; shift -= 8) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < 256; i += THREADS) bins[i] = 0;
+            __syncthreads();
+            // equal digits follow each other in such rows, and are added once
+            int32_t digit = 0, length = 0;
             z.again().each(none, [&](const Eight &v, int32_t c, uint32_t) {
 #pragma unroll
-                for (int i = 0; i < 8; i++) sum += wanted(ordered(v.v[i]), c + i) ? 1.0f : 0.0f;
+                for (int i = 0; i < 8; i++) {
+                    const uint64_t one = key_of(v.v[i], c + i);
+                    if (one >> 24 == 0 || one >> (shift + 8) != key >> (shift + 8)) continue;
+                    const int32_t next = (int32_t)(one >> shift & 255);
+                    if (next != digit) {
+                        if (length) atomicAdd(&bins[digit], length);
+                        digit = next, length = 0;
+                    }
+                    length++;
+                }
             });
-            return (int32_t)over.sum(sum);        // (whole numbers below 2^24)
-        };
-        uint32_t key = 0, column = 0;             // of the k-th
-        for (int bit = 31; bit >= 0; bit--) {
-            const uint32_t next = key | 1u << bit;
-            if (count([&](uint32_t v, int32_t) { return v >= next; }) >= a.k) key = next;
-        }
-        const int32_t equal = a.k - count([&](uint32_t v, int32_t) { return v > key; });
-        for (int bit = 19; bit >= 0; bit--) {
-            const uint32_t next = column | 1u << bit;
-            if (count([&](uint32_t v, int32_t c) { return v == key && (uint32_t)c < next; }) < equal) column = next;
+            if (length) atomicAdd(&bins[digit], length);
+            __syncthreads();
+            // four digits a lane, the highest first: how many have its or a higher one
+            int32_t of[4], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; i++) of[i] = bins[255 - (lane * 4 + i)], sum += of[i];
+            const int32_t all = wave_scan(sum);
+            const int from = __builtin_ctzll(__ballot(all >= left));      // (as many as are wanted there are)
+            int32_t above = __builtin_amdgcn_readlane(all - sum, from);
+            int at = 0;
+#pragma unroll
+            for (int i = 0; i < 3; i++) {
+                const int32_t more = __builtin_amdgcn_readlane(of[i], from);
+                if (at == i && above + more < left) above += more, at++;
+            }
+            key |= (uint64_t)(255 - (from * 4 + at)) << shift;
+            int32_t same = 0;
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (at == i) same = __builtin_amdgcn_readlane(of[i], from);
+            n = a.k - left + above + same;
+            left -= above;
         }
         __syncthreads();
         if (threadIdx.x == 0) used = 0;
         __syncthreads();
         z.again().each(none, [&](const Eight &v, int32_t c, uint32_t) {
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                const uint32_t one = ordered(v.v[i]);
-                if (one > key || (one == key && (uint32_t)(c + i) <= column)) put(v.v[i], c + i);
-            }
+            for (int i = 0; i < 8; i++)
+                if (v.v[i] > -INFINITY && key_of(v.v[i], c + i) >= key) put(v.v[i], c + i);
         });
         __syncthreads();
         n = used;
     }
+    if constexpr (WAVES <= 4)
+        if (n > kFew && n > 2 * a.k) {
+            uint32_t values[kRoom / 64], least = 0;
+#pragma unroll
+            for (int i = 0; i < kRoom / 64; i++) values[i] = i * 64 + lane < n ? (uint32_t)(found[i * 64 + lane] >> 32) : 0u;
+            for (int bit = 31; bit >= 0; bit--) {
+                const uint32_t next = least | 1u << bit;
+                int count = 0;
+#pragma unroll
+                for (int i = 0; i < kRoom / 64; i++)
+                    if (i * 64 < n) count += __popcll(__ballot(values[i] >= next));
+                if (count >= a.k) least = next;
+            }
+            uint64_t mine[kRoom / THREADS];
+#pragma unroll
+            for (int i = 0; i < kRoom / THREADS; i++) mine[i] = i * THREADS + (int)threadIdx.x < n ? found[i * THREADS + threadIdx.x] : 0u;
+            __syncthreads();
+            if (threadIdx.x == 0) used = 0;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kRoom / THREADS; i++)
+                if (mine[i] && (uint32_t)(mine[i] >> 32) >= least) found[atomicAdd(&used, 1)] = mine[i];
+            __syncthreads();
+            n = used;
+        }
 
     // places past the list's end are the lowest, up to whole groups of them that are read together
     constexpr int kTogether = 8;
@@ -218,17 +275,22 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     if (threadIdx.x == 0) a.rest[row] = from * a.per_T + logf(sum);
 }
 
-// As distill.hip's.
+// launch(wavefronts of a row, packs of eight that a lane holds).  Many rows go by as few wavefronts as hold them, which have fewer barriers and
+// rounds over LDS to share (us, bf16, k = 32; 16384 x 1000 by 1 wavefront of 2 packs 20.8, by 2 of 1 33.8; x 2000 by 1 of 4 32.2, by 4 of 2
+// 58.7; 15625 x 16000 by 4 of 8 132, by 8 of 4 144; 4997 x 50021 by 8 of 16 180, by 16 of 8 275, read again and again 237), a few rows by as
+// many as shorten their way (128 x 2000 7.9, 5.8; x 16000 9.5, 8.2; x 64000 15.3, 14.0).  Of one wavefront's 64 largest values, or two's 128, a
+// bound for many is too low (8192 x 2000, k = 64: 37 by one, 29 by four; x 4000, k = 128: 85 by two, 54 by four).  fp32 rows of more than
+// 65536 columns are not held (1923 x 130000 335, held 551).
 template <class T, class F>
-int by_columns(int64_t columns, int64_t rows, F launch)
+int by_columns(int64_t columns, int64_t rows, int k, F launch)
 {
     using std::integral_constant;
     const int64_t packs = (columns + 7) / 8;
     const bool few = rows <= 256;
     if (packs <= 64) return launch(integral_constant<int, 1>(), integral_constant<int, 1>());
     if (packs <= 128) return launch(integral_constant<int, 1>(), integral_constant<int, 2>());
-    if (packs <= 256 && !few) return launch(integral_constant<int, 1>(), integral_constant<int, 4>());
-    if (packs <= 512) return few ? launch(integral_constant<int, 4>(), integral_constant<int, 2>()) : launch(integral_constant<int, 2>(), integral_constant<int, 4>());
+    if (packs <= 256 && !few && k <= 48) return launch(integral_constant<int, 1>(), integral_constant<int, 4>());
+    if (packs <= 512) return few || k > 96 ? launch(integral_constant<int, 4>(), integral_constant<int, 2>()) : launch(integral_constant<int, 2>(), integral_constant<int, 4>());
     if (packs <= 1024) return launch(integral_constant<int, 4>(), integral_constant<int, 4>());
     if (packs <= 2048) return few ? launch(integral_constant<int, 8>(), integral_constant<int, 4>()) : launch(integral_constant<int, 4>(), integral_constant<int, 8>());
     if (packs <= 4096) return few ? launch(integral_constant<int, 16>(), integral_constant<int, 4>()) : launch(integral_constant<int, 8>(), integral_constant<int, 8>());
@@ -241,7 +303,7 @@ int by_columns(int64_t columns, int64_t rows, F launch)
 template <class T>
 int run_top(const TopArgs &a, int64_t rows, hipStream_t st)
 {
-    return by_columns<T>(a.columns, rows, [&](auto waves, auto packs) -> int {
+    return by_columns<T>(a.columns, rows, a.k, [&](auto waves, auto packs) -> int {
         constexpr int W = decltype(waves)::value, P = decltype(packs)::value;
         if (!fits_launch((uint64_t)rows * 64 * W)) return CCDC_ESIZE;
         k_top<T, W, P><<<(uint32_t)rows, 64 * W, 0, st>>>(a);

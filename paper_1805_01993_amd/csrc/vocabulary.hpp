@@ -24,6 +24,21 @@ __device__ __forceinline__ float wave_most(float v)
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
+// The sum of a lane's and all lanes' before it.
+__device__ __forceinline__ int32_t wave_scan(int32_t v)
+{
+    const auto moved = [](int32_t x, auto control, auto rows) {
+        return __builtin_amdgcn_update_dpp(0, x, decltype(control)::value, decltype(rows)::value, 15, true);
+    };
+    using std::integral_constant;
+    v += moved(v, integral_constant<int, 0x111>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x112>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x114>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x118>(), integral_constant<int, 15>());
+    v += moved(v, integral_constant<int, 0x142>(), integral_constant<int, 10>());
+    return v + moved(v, integral_constant<int, 0x143>(), integral_constant<int, 12>());
+}
+
 // exp((v - from) / T) as a power of two, in one product and sum: 2^(v scale - K) with K = from scale rounded.  What K is off by is
 // exact as a product and sum again, below one while K is below 2^24, and `lost` undoes it in a sum of these.  Rows further from zero
 // (those of which the lowest number of the type is the largest, say) are `far`: there the difference is taken first.

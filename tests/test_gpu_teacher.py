@@ -576,6 +576,22 @@ def test_largest_rows(blocks):
 
 
 @pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("columns", [300, 520, 1000, 2000, 4000, 20000, 50021])
+def test_much_wanted_of_rows(blocks, mode, columns):
+    """As many as the list may have: of short rows, where many columns reach any bound, and of rows with equal values, which are listed
+    by their columns."""
+    random = noise(columns, 12, columns)
+    coarse = (random * 2).round()
+    few = torch.full_like(random, torch.finfo(R.DTYPES[mode]).min)
+    few[:, [7, 33, columns - 1]] = random[:, :3]
+    last = torch.zeros_like(random)
+    last[:, -100:] = 1.0
+    for z in (random, coarse, few, last, random * 0.0, -coarse.abs(), random.sort(1).values):
+        for k in (33, 49, 65, 97, 128):
+            check_top(blocks[mode], z.to(R.DTYPES[mode]).cuda(), k)
+
+
+@pytest.mark.parametrize("mode", MODES)
 @pytest.mark.parametrize("columns", [524288, 524289, 1 << 20])
 def test_long_rows(blocks, mode, columns):
     """Rows that are held in part, and those of which none is: more bits of listed columns than leave room for it."""
