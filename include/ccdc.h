@@ -451,7 +451,8 @@ int ccdc_packed_product(const ccdc_block_t *block, int64_t rows, int64_t outputs
 /* The k largest of each row of z [rows][columns], 1 <= k <= 128: index [rows][k] their columns and value [rows][k] themselves, larger
  * ones first and of equal ones the lower column.  What is -infinity (masked) or a NaN is not among them; where a row has fewer, index is
  * -1 and value -infinity.  rest [rows] (NULL: not wanted): the logarithm of the sum of exp(z / temperature) over all other
- * columns, -infinity where there are none; a NaN in the row makes it one.  CCDC_ESIZE for columns above 2^20. */
+ * columns, -infinity where there are none; a NaN in the row makes it one.  CCDC_EINVAL for a temperature that is not above zero, or so
+ * near it that 1.5 / temperature is no fp32 number; CCDC_ESIZE for columns above 2^20. */
 int ccdc_top(const ccdc_block_t *block, int64_t rows, int64_t columns, const void *z, int64_t ldz, int k, double temperature,
              int32_t *index, float *value, float *rest, void *stream);
 
@@ -465,8 +466,8 @@ int ccdc_top(const ccdc_block_t *block, int64_t rows, int64_t columns, const voi
  * entropy of a label.  weight [rows] (NULL: ones): a row of weight 0 has zeros, whatever its logits.  An entry with an
  * index outside 0 .. columns - 1, or that of an entry before it, is none; a row without entries, or whose values (and
  * rest) or logits are all -infinity, has nothing to learn: zeros.  A term with p = 0 is 0.  A NaN or +infinity among the logits makes the row's results NaN.
- * loss [rows] and dz [rows][columns] may be NULL: not wanted (not both).  dz may be z (then lddz = ldz).  CCDC_ESIZE for columns
- * above 2^20. */
+ * loss [rows] and dz [rows][columns] may be NULL: not wanted (not both).  dz may be z (then lddz = ldz).  Temperatures
+ * as ccdc_top's; CCDC_EINVAL for a scale that is no fp32 number, CCDC_ESIZE for columns above 2^20. */
 int ccdc_distill(const ccdc_block_t *block, int64_t rows, int64_t columns, const void *z, int64_t ldz, int k, const int32_t *index,
                  const float *value, const float *rest, double temperature, const float *weight, double scale, float *loss,
                  void *dz, int64_t lddz, void *stream);

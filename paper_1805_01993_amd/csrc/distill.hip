@@ -295,7 +295,7 @@ int ccdc_distill(const ccdc_block_t *b, int64_t rows, int64_t columns, const voi
     if (rc != CCDC_OK) return rc;
     if (rows < 0 || columns < 1 || ldz < columns || k < 1 || k > kMostListed || (dz && lddz < columns)) return CCDC_EINVAL;
     const float heat = (float)temperature, per_T = 1.0f / heat;
-    if (!(heat > 0.0f) || !std::isfinite(heat) || !std::isfinite(per_T) || !std::isfinite((float)scale)) return CCDC_EINVAL;
+    if (!(heat > 0.0f) || !std::isfinite(heat) || !std::isfinite(per_T * kLog2e) || !std::isfinite((float)scale)) return CCDC_EINVAL;
     if (rows == 0) return CCDC_OK;
     if (!loss && !dz) return CCDC_EINVAL;
     if (!fits(b, z) || !fits(b, dz, true) || !index || !value || (dz && dz == z && lddz != ldz)) return CCDC_EINVAL;

@@ -260,7 +260,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     }
     auto again = z.again();
     const auto sum_from = [&] {
-        return sum_of(again, [&](float v, int32_t c) { return __builtin_amdgcn_exp2f((not_listed(v, c) - from) * scale); });
+        return sum_of(again, [&](float v, int32_t c) {
+            const float other = not_listed(v, c);             // (an infinity like `from` is one too)
+            return other == from ? 1.0f : __builtin_amdgcn_exp2f((other - from) * scale);
+        });
     };
     if (sum == 0.0f) sum = sum_from();            // (the same for all threads)
     if (sum < 1e-30f) {
@@ -322,7 +325,7 @@ int ccdc_top(const ccdc_block_t *b, int64_t rows, int64_t columns, const void *z
     if (rc != CCDC_OK) return rc;
     if (rows < 0 || columns < 1 || ldz < columns || k < 1 || k > kMostListed) return CCDC_EINVAL;
     const float heat = (float)temperature, per_T = 1.0f / heat;
-    if (!(heat > 0.0f) || !std::isfinite(heat) || !std::isfinite(per_T)) return CCDC_EINVAL;
+    if (!(heat > 0.0f) || !std::isfinite(heat) || !std::isfinite(per_T * kLog2e)) return CCDC_EINVAL;
     if (rows == 0) return CCDC_OK;
     if (!fits(b, z) || !index || !value) return CCDC_EINVAL;
     for (const void *p : {(const void *)index, (const void *)value, (const void *)rest})

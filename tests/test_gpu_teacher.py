@@ -592,6 +592,31 @@ def test_much_wanted_of_rows(blocks, mode, columns):
 
 
 @pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("columns", [100, 1000, 9000, 70000])
+def test_infinities_among_the_others(blocks, mode, columns):
+    """More infinities than the list takes: the others' sum is one; a NaN beside them makes it none."""
+    z = noise(3, 5, columns)
+    z[0, [3, 50, columns - 1]] = math.inf
+    z[1, ::2] = math.inf
+    z[2, 5:] = math.inf
+    z[3, [3, 50, columns - 1]], z[3, 77] = math.inf, math.nan
+    z[4, 4] = math.inf
+    for k in (1, 2, 3, 4):
+        check_top(blocks[mode], z.to(R.DTYPES[mode]).cuda(), k)
+
+
+def test_temperatures_of_no_power(blocks):
+    """1 / temperature is a number, and times log2(e) not."""
+    import paper_1805_01993_amd as L
+    block, z = blocks["f32"], torch.zeros(1, 8, device="cuda")
+    index, value = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.zeros(1, 1, device="cuda")
+    for call in (lambda: block.top(z, index, value, temperature=3.5e-39),
+                 lambda: block.distill(z, index, value, value[0], None, temperature=3.5e-39)):
+        with pytest.raises(L.CcdcError):
+            call()
+
+
+@pytest.mark.parametrize("mode", MODES)
 @pytest.mark.parametrize("columns", [524288, 524289, 1 << 20])
 def test_long_rows(blocks, mode, columns):
     """Rows that are held in part, and those of which none is: more bits of listed columns than leave room for it."""
