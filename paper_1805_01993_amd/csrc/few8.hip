@@ -12,6 +12,12 @@
 // From 9 rows on LDS's copies are worth their way where the weights have many rows (16 rows of 4096 x 11264: 15.3 us here, 14.6 by
 // tiles of 64 x 64; of 1600 x 32768 15.3, 12.4; of 11264 x 4096 13.7, 32), with fp32 results not (15.4, 21.9).  Loads of a next
 // step begun before this one's products lost more by those past the rows' ends than they gave (14.8 us).
+// Of few outputs there are fewer workgroups than CUs, and more than 16 rows are divided among workgroups too: a group of 8 or 16 outputs
+// for 8, 16 or 32 rows, whichever leaves a CU the least to read.  64 rows of 11264 x 1024 12.2 us by 16 x 16 (16 x 32 18.2, 8 x 8 22.4, tiles of
+// 64 x 64 31.5), x 2048 19.3 by 16 x 32 (32.0 by tiles), x 4096 25.0 by 32 x 32 (34.0), x 6000 34.6 by tiles (45.4); 16 rows of 11264 x
+// 1024 7.2 by 8 x 8, 12.1 by 16 x 16.
+#include <algorithm>
+
 #include "eight.hpp"
 
 namespace {
@@ -77,12 +83,12 @@ __global__ __launch_bounds__(64 * WAVES) void k_few8(const Product8Args a)
     constexpr int R = 16 / S, COLUMNS = MT * R;
     __shared__ float sums[WAVES][G][MT][16][17];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, part = r % S;
-    const int32_t n0 = blockIdx.x * (R * G), B = ((a.blocks + S - 1) / S + 3) / 4 * 4, first = part * B;
+    const int32_t n0 = blockIdx.x * (R * G), m0 = blockIdx.y * COLUMNS, B = ((a.blocks + S - 1) / S + 3) / 4 * 4, first = part * B;
     Line w[G], x[MT];
 #pragma unroll
     for (int g = 0; g < G; g++) w[g].set(a.n, a.n_scale, min(n0 + g * R + r / S, a.rows_n - 1), a);
 #pragma unroll
-    for (int t = 0; t < MT; t++) x[t].set(a.m, a.m_scale, min(t * R + r / S, a.rows_m - 1), a);
+    for (int t = 0; t < MT; t++) x[t].set(a.m, a.m_scale, min(m0 + t * R + r / S, a.rows_m - 1), a);
     Acc4 acc[G][MT] = {};
     for (int32_t s = wave * NB; s < B; s += WAVES * NB) {
         int32_t block[NB];
@@ -132,13 +138,13 @@ __global__ __launch_bounds__(64 * WAVES) void k_few8(const Product8Args a)
     __syncthreads();
     for (int o = threadIdx.x; o < R * G * COLUMNS; o += 64 * WAVES) {
         const int n = o % (R * G), c = o / (R * G), in = n % R;
-        if (n0 + n >= a.rows_n || c >= a.rows_m) continue;
+        if (n0 + n >= a.rows_n || m0 + c >= a.rows_m) continue;
         float total = 0.0f;
 #pragma unroll
         for (int v = 0; v < WAVES; v++)
 #pragma unroll
             for (int p = 0; p < S; p++) total += sums[v][n / R][c * S / 16][in * S + p][c * S % 16 + p];
-        ((E *)a.c)[c * a.ldc + n0 + n] = narrow<T>(total);
+        ((E *)a.c)[(m0 + c) * a.ldc + n0 + n] = narrow<T>(total);
     }
 }
 
@@ -147,9 +153,9 @@ int run_few8(const Product8Args &a, hipStream_t st)
 {
     const auto go = [&](auto s, auto mt, auto waves, auto g, auto nb) -> int {
         constexpr int S = decltype(s)::value, MT = decltype(mt)::value, WAVES = decltype(waves)::value, G = decltype(g)::value, NB = decltype(nb)::value;
-        const uint32_t blocks = cdiv(a.rows_n, 16 / S * G);
-        if (!fits_launch((uint64_t)blocks * 64 * WAVES)) return CCDC_ESIZE;
-        k_few8<T, S, MT, WAVES, G, NB><<<blocks, 64 * WAVES, 0, st>>>(a);
+        const uint32_t blocks = cdiv(a.rows_n, 16 / S * G), rows = cdiv(a.rows_m, 16 / S * MT);
+        if (!fits_launch((uint64_t)blocks * rows * 64 * WAVES)) return CCDC_ESIZE;
+        k_few8<T, S, MT, WAVES, G, NB><<<dim3(blocks, rows), 64 * WAVES, 0, st>>>(a);
         return launched();
     };
     using std::integral_constant;
@@ -160,9 +166,13 @@ int run_few8(const Product8Args &a, hipStream_t st)
     const bool wide = a.rows_n >= 8192;               // with two groups a workgroup there still are enough workgroups
     if (a.rows_m <= 4 && a.rows_n < 2048) return go(four, one, four, one, two);
     if (a.rows_m <= 8) return wide ? go(two, one, eight, two, two) : go(two, one, eight, one, two);
-    if (a.rows_m <= 16) return wide ? go(one, one, four, four, two) : go(one, one, eight, one, two);
-    if (a.rows_m <= 32) return wide ? go(one, two, eight, two, two) : go(one, two, eight, one, two);
-    return go(one, four, eight, one, two);
+    if (wide && a.rows_m <= 32) return a.rows_m <= 16 ? go(one, one, four, four, two) : go(one, two, eight, two, two);
+    // the fewest rows, of both sides, that a CU has to read (what it takes from L2 or memory is some 45 GB/s)
+    const auto read = [&](uint32_t n, uint32_t m) { return cdiv((uint64_t)cdiv(a.rows_n, n) * cdiv(a.rows_m, m), 256) * (n + m); };
+    const auto small = read(8, 8), square = read(16, 16), tall = read(16, 32), large = read(32, 32), least = std::min(std::min(small, square), std::min(tall, large));
+    if (square == least) return go(one, one, eight, one, two);
+    if (small == least) return go(two, one, eight, one, two);
+    return tall == least ? go(one, two, eight, one, two) : go(one, two, eight, two, two);
 }
 
 }  // namespace
@@ -174,7 +184,7 @@ bool few_rows8(const ccdc_block_t *b, const Product8Args &a)
     if (a.rows_m > 64 || a.blocks < 8) return false;
     if (a.rows_m <= 8) return true;
     if (a.rows_m <= 32) return a.rows_n < 8192 || b->planes == 3;
-    return a.rows_n <= 2048;
+    return a.rows_n <= 4096;
 }
 
 int few_product8(const ccdc_block_t *b, const Product8Args &a, hipStream_t st) { CCDC_BY_ELEM(b, (run_few8<T>(a, st))); }

@@ -142,6 +142,21 @@ def test_product_of_few_rows(blocks, mode, rows, wide, outputs):
 
 
 @pytest.mark.parametrize("mode", MODES)
+@pytest.mark.parametrize("rows", [9, 16, 17, 31, 33, 47, 64])
+@pytest.mark.parametrize("outputs", [7, 500, 1021, 1500, 2048, 4093, 4100])
+def test_product_of_few_rows_divided_among_workgroups(blocks, mode, rows, outputs):
+    """Groups of 8, 16 and 32 rows, the last of them not full; what is next to the result stays."""
+    x, xs = random_packed(rows, rows, 1152)
+    w, ws = random_packed(outputs, outputs, 1152)
+    y, room = guarded(rows, outputs, R.DTYPES[mode], 1)
+    blocks[mode].packed_product(x, xs, w, ws, y)
+    torch.cuda.synchronize()
+    assert untouched(room, y)
+    want, off = R.product(R.values(x, xs), R.values(w, ws), mode)
+    assert bool(((y.double().cpu() - want).abs() <= off).all()), float(((y.double().cpu() - want).abs() / off).max())
+
+
+@pytest.mark.parametrize("mode", MODES)
 @pytest.mark.parametrize("rows,wide,outputs", [(2049, 128, 4100), (4096, 256, 2304), (1030, 384, 5003), (700, 2304, 900)])
 def test_products_of_many_tiles(blocks, mode, rows, wide, outputs):
     """Tiles of both sizes, with edges; compared where the definition is affordable: some rows, some columns."""
