@@ -234,7 +234,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
     __syncthreads();
     // What is not listed is at most the last that is, which is what it is summed from.  All columns are, none as more than that last: the
     // k that are listed are then ones, and where half of the sum is left without them it has lost a bit.  Else the listed ones are left
-    // out one by one, and where fp32 has nothing of the others so far below the list, it is from their own largest.
+    // out one by one: from the last listed still where the others come to more than two of it, from their own largest where they may be any
+    // distance below it: a sum of packs has to have a one among them (PackSum), or others that lie 15 T and more below the last listed are rounded
+    // away, all of them or some.  Such rows are gone through twice more (us, bf16, 4096 x 50021, k = 64: 140 where the sum is
+    // left, 227 from the last listed, 259 from the others' largest; 512 x 130000 fp32, read again each time: 80 and 156).
     const uint64_t kth = last;
     const float least = kth ? value_of((uint32_t)(kth >> 32)) : -INFINITY, scale = a.per_T * kLog2e;
     const int32_t column = kth ? (int32_t)(0xFFFFFFFFu - (uint32_t)kth) : -1;
@@ -251,29 +254,30 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
         });
         return over.sum(sum);
     };
+    bool lost = true, near = false;               // (the same for all threads)
     if (kth && !powers.far()) {
         // (a NaN is the smaller of two numbers here: one instruction, where a comparison and a choice are two)
         const float one = fmaf(least, scale, -powers.K);
         sum = sum_of(z, [&](float v, int32_t) { return __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(fmaf(v, scale, -powers.K), one)); });
         const float listed = (float)a.k * powers(least);
-        sum = sum - listed < listed ? 0.0f : (sum - listed) * powers.lost();
+        lost = sum - listed < listed;
+        sum = (sum - listed) * powers.lost();
+        near = sum >= 2.0f;
     }
-    auto again = z.again();
-    const auto sum_from = [&] {
-        return sum_of(again, [&](float v, int32_t c) {
+    if (lost) {
+        auto again = z.again();
+        if (!near) {
+            float own_most = -INFINITY;
+            z.each(none, [&](const Eight &v, int32_t c, uint32_t) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) own_most = fmaxf(own_most, not_listed(v.v[i], c + i));
+            });
+            from = fmaxf(over.most(own_most), kLowest);
+        }
+        sum = sum_of(again, [&](float v, int32_t c) {
             const float other = not_listed(v, c);             // (an infinity like `from` is one too)
             return other == from ? 1.0f : __builtin_amdgcn_exp2f((other - from) * scale);
         });
-    };
-    if (sum == 0.0f) sum = sum_from();            // (the same for all threads)
-    if (sum < 1e-30f) {
-        float own_most = -INFINITY;
-        again.each(none, [&](const Eight &v, int32_t c, uint32_t) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) own_most = fmaxf(own_most, not_listed(v.v[i], c + i));
-        });
-        from = fmaxf(over.most(own_most), kLowest);
-        sum = sum_from();
     }
     if (threadIdx.x == 0) a.rest[row] = from * a.per_T + logf(sum);
 }

@@ -73,8 +73,9 @@ __device__ __forceinline__ double wave_sum(double v)
 }
 
 // A sum of the packs of a row that is the same whatever thread has which of them: in 64 bits, of numbers rounded to 2^-32, which is exact
-// up to 2^21 (a pack is at most 8 exponentials of at most 2^(1/2), of 2^17 packs).  The roundings are 2^-33 a pack where the sum is one
-// or more.  Four instructions a pack of eight.
+// up to 2^21 (a pack is at most 8 exponentials of at most 2^(1/2), of 2^17 packs).  The roundings are 2^-33 a pack, of a sum that has to be
+// one or so at least (2^(-1/2)): whoever sums takes exponentials from the largest of what is summed, or knows of as much.  Four
+// instructions a pack of eight.
 struct PackSum {
     double sum = 0.0;
     __device__ __forceinline__ void add(float pack)

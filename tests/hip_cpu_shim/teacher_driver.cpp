@@ -3,7 +3,9 @@
 // what lies between its rows is poisoned; results begin as what no result is.  Test infrastructure only.
 // Usage: teacher_driver quantise MODE ROWS COLUMNS PAD
 //        teacher_driver product MODE ROWS WIDE OUTPUTS PAD TILE       (TILE: shim::force)
-//        teacher_driver top MODE ROWS COLUMNS K PAD KIND              (KIND 0 noise, 1 all equal, 2 masked but for few)
+//        teacher_driver top MODE ROWS COLUMNS K PAD KIND              (KIND 0 noise, 1 all equal, 2 masked but for few,
+//                                                                      10 ... all but the last K that many T below them,
+//                                                                      -10 ... one of these, the others 5 T further down)
 //        teacher_driver distill MODE ROWS COLUMNS K PAD PLACE         (PLACE 1: dz is z)
 #include <sanitizer/asan_interface.h>
 
@@ -151,6 +153,14 @@ void product(ccdc_block_t *b, int64_t rows, int64_t wide, int64_t outputs, int64
         }
 }
 
+// K logits of zero at a row's end, the others far below them.
+void logits_apart(const Room &z, int kind, int k, double T)
+{
+    const int64_t above = std::max<int64_t>(z.columns - k, 0);
+    for (int64_t i = 0; i < z.rows; i++)
+        for (int64_t j = 0; j < z.columns; j++) put(z.at(i, j), j >= above ? 0.0 : -T * (kind > 0 ? kind : j == above / 2 ? -kind : 5 - kind));
+}
+
 void logits(const Room &z, int kind)
 {
     for (int64_t i = 0; i < z.rows; i++)
@@ -160,8 +170,10 @@ void logits(const Room &z, int kind)
 void top(ccdc_block_t *b, int64_t rows, int64_t columns, int k, int64_t pad, int kind)
 {
     Room z(rows, columns, pad, elem()), index(rows, k, 0, 4), value(rows, k, 0, 4), rest(rows, 1, 0, 4);
-    logits(z, kind);
     const double T = 1.5;
+    const bool apart = std::abs(kind) >= 10;
+    if (apart) logits_apart(z, kind, k, T);
+    else logits(z, kind);
     CHECK(ccdc_top(b, rows, columns, z.p, z.ld, k, T, (int32_t *)index.p, (float *)value.p, (float *)rest.p, nullptr));
     for (int64_t i = 0; i < rows; i++) {
         std::vector<int32_t> order;
@@ -175,7 +187,8 @@ void top(ccdc_block_t *b, int64_t rows, int64_t columns, int k, int64_t pad, int
             else sum += std::exp(v / T);
         }
         for (int j = (int)order.size(); j < k; j++) near("index", i, j, index.as<int32_t>(i, j), -1, 0), near("value", i, j, value.as<float>(i, j), -INFINITY, 0);
-        near("rest", i, 0, rest.as<float>(i), std::log(sum), 2e-5);
+        // (far from zero: what is summed from by 1 / T, both rounded, and the logarithm's sum with it)
+        near("rest", i, 0, rest.as<float>(i), std::log(sum), 2e-5 + (apart ? 4 * 0x1p-24 * std::fabs(std::log(sum)) : 0.0));
     }
 }
 
