@@ -27,11 +27,9 @@ typedef float Acc4 __attribute__((ext_vector_type(4)));
 
 struct Block8 {
     Bytes32 q;
-    int scale;
+    int scale;                            // in its lowest byte
 };
 
-// fp32 results: the numbers as bfloat16 with their scale, whose products the instructions add in fp32 (ccdc.h has what they drop in
-// 8 bits, 2^-14 or so of a result).
 template <class T>
 __device__ __forceinline__ Acc4 multiply(const Block8 &n, const Block8 &m, Acc4 c)
 {
@@ -46,6 +44,19 @@ __device__ __forceinline__ Acc4 multiply(const Block8 &n, const Block8 &m, Acc4 
     }
 }
 
+// The same where scales leave bfloat16's range.
+__device__ __forceinline__ Acc4 multiply_in_turns(const Block8 &n, const Block8 &m, Acc4 c)
+{
+#pragma unroll 1
+    for (int turn = 0; turn < kScaleTurns; turn++) {
+        const ScaleInTurn sn = scale_in_turn(n.scale, true, turn), sm = scale_in_turn(m.scale, false, turn);
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide_in_turn(n.q[2 * i], n.q[2 * i + 1], sn), wide_in_turn(m.q[2 * i], m.q[2 * i + 1], sm), c, 0, 0, 0);
+    }
+    return c;
+}
+
 // One row's share of a lane: its numbers and scales.
 struct Line {
     const uint8_t *q, *scale;
@@ -53,6 +64,14 @@ struct Line {
     {
         q = base + row * a.ld + threadIdx.x % 64 / 16 * 16;
         scale = scales + row * a.ld_scale;
+    }
+    // One block by itself; past the end as k_few8 has it.
+    __device__ __forceinline__ Block8 block(int32_t b, const Product8Args &a) const
+    {
+        const uint8_t *p = q + (int64_t)min(b, a.blocks - 1) * 128;
+        Block8 o{both(*(const Bytes16 *)p, *(const Bytes16 *)(p + 64)), scale[min(b, a.blocks - 1)]};
+        if (b >= a.blocks) o = {Bytes32{}, 127};
+        return o;
     }
 };
 
@@ -90,6 +109,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_few8(const Product8Args a)
 #pragma unroll
     for (int t = 0; t < MT; t++) x[t].set(a.m, a.m_scale, min(m0 + t * R + r / S, a.rows_m - 1), a);
     Acc4 acc[G][MT] = {};
+    ScalesSeen seen;
     for (int32_t s = wave * NB; s < B; s += WAVES * NB) {
         int32_t block[NB];
 #pragma unroll
@@ -122,12 +142,32 @@ __global__ __launch_bounds__(64 * WAVES) void k_few8(const Product8Args a)
 #pragma unroll
                 for (int t = 0; t < MT; t++) keep(ox[t]);
             }
+            if constexpr (T::planes == 3) {
+#pragma unroll
+                for (int g = 0; g < G; g++) seen.see(ow[g].scale & 255);
+#pragma unroll
+                for (int t = 0; t < MT; t++) seen.see(ox[t].scale & 255);
+            }
 #pragma unroll
             for (int g = 0; g < G; g++)
 #pragma unroll
                 for (int t = 0; t < MT; t++) acc[g][t] = multiply<T>(ow[g], ox[t], acc[g][t]);
         }
     }
+    if constexpr (T::planes == 3)
+        if (seen.others()) {
+#pragma unroll
+            for (int g = 0; g < G; g++)
+#pragma unroll
+                for (int t = 0; t < MT; t++) {
+                    Acc4 sum = {};
+#pragma unroll 1
+                    for (int32_t s = wave * NB; s < B; s += WAVES * NB)
+#pragma unroll 1
+                        for (int b = 0; b < NB; b++) sum = multiply_in_turns(w[g].block(first + s + b, a), x[t].block(first + s + b, a), sum);
+                    acc[g][t] = sum;
+                }
+        }
     // lane l has rows 4 (l / 16) ... of column l % 16
 #pragma unroll
     for (int g = 0; g < G; g++)

@@ -79,7 +79,7 @@ __device__ __forceinline__ void multiply(Acc (&acc)[SN][SM], const Bytes32 (&n)[
             for (int j = 0; j < COUNT; j++)
                 acc[i][FROM + j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(n[i], m[j], acc[i][FROM + j], 0, 0, 0, sn[i], 0, sm[FROM + j]);
     } else {
-        // fp32 results: as bfloat16 with the scales (few8.hip)
+        // fp32 results: as bfloat16 with the scales (eight.hpp)
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             Wide8 wn[SN], wm[COUNT];
@@ -93,6 +93,28 @@ __device__ __forceinline__ void multiply(Acc (&acc)[SN][SM], const Bytes32 (&n)[
                 for (int j = 0; j < COUNT; j++) acc[i][FROM + j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wn[i], wm[j], acc[i][FROM + j], 0, 0, 0);
         }
     }
+}
+
+// 32 x 32 sums from memory, a lane's row of either side given, as `multiply` adds them, where scales leave bfloat16's range.
+__device__ __forceinline__ Acc sum_in_turns(const Product8Args &a, int32_t row_n, int32_t row_m)
+{
+    const uint32_t pack = threadIdx.x % 64 / 32 * 16;
+    const uint8_t *n = a.n + (int64_t)row_n * a.ld + pack, *m = a.m + (int64_t)row_m * a.ld + pack;
+    const uint8_t *n_scale = a.n_scale + (int64_t)row_n * a.ld_scale, *m_scale = a.m_scale + (int64_t)row_m * a.ld_scale;
+    Acc sum = {};
+#pragma unroll 1
+    for (int32_t s = 0; s < a.blocks * 2; s++) {              // halves of a block, as `piece` has them
+        const Bytes32 bn = both(*(const Bytes16 *)(n + (int64_t)s * 64), *(const Bytes16 *)(n + (int64_t)s * 64 + 32));
+        const Bytes32 bm = both(*(const Bytes16 *)(m + (int64_t)s * 64), *(const Bytes16 *)(m + (int64_t)s * 64 + 32));
+#pragma unroll 1
+        for (int turn = 0; turn < kScaleTurns; turn++) {
+            const ScaleInTurn sn = scale_in_turn(n_scale[s / 2], true, turn), sm = scale_in_turn(m_scale[s / 2], false, turn);
+#pragma unroll
+            for (int q = 0; q < 4; q++)
+                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wide_in_turn(bn[2 * q], bn[2 * q + 1], sn), wide_in_turn(bm[2 * q], bm[2 * q + 1], sm), sum, 0, 0, 0);
+        }
+    }
+    return sum;
 }
 
 // WN x WM wavefronts, each SN x SM pieces; BUFFERS steps in LDS.
@@ -159,6 +181,7 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product8(const Product8Args a)
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     };
     int sn[SN], sm[SM];
+    ScalesSeen seen;
     if constexpr (SM == 4) {
         static_assert(THREADS == 512);
         // Two wavefronts a SIMD, the second of each a phase behind, in turns at reading pieces and multiplying them (product.hip).
@@ -244,6 +267,12 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product8(const Product8Args a)
             for (int j = 0; j < SM; j++) sm[j] = next_m[j];
             read(1, s, 1);
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (T::planes == 3) {
+#pragma unroll
+                for (int i = 0; i < SN; i++) seen.see(sn[i]);
+#pragma unroll
+                for (int j = 0; j < SM; j++) seen.see(sm[j]);
+            }
             multiply<T, SN, SM, 0, SM>(acc, pn[0], pm[0], sn, sm);
             __builtin_amdgcn_sched_barrier(0);
             // also after the last step, and what is read then is not used (product.hip)
@@ -259,6 +288,13 @@ __global__ __launch_bounds__(64 * WN * WM) void k_product8(const Product8Args a)
     // what was read last is not used, and other wavefronts' reads of it are over before it is written over
     reads_there();
     meet();
+    if constexpr (T::planes == 3)
+        if (seen.others())
+#pragma unroll
+            for (int i = 0; i < SN; i++)
+#pragma unroll
+                for (int j = 0; j < SM; j++)
+                    acc[i][j] = sum_in_turns(a, min(tile_n + wn + i * 32 + lane % 32, a.rows_n - 1), min(tile_m + wm + j * 32 + lane % 32, a.rows_m - 1));
 
     // The result goes through LDS, a wavefront's rows of 64 n at a time, each by itself (product.hip).
     static_assert(SN == 2);

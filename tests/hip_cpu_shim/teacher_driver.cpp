@@ -3,6 +3,7 @@
 // what lies between its rows is poisoned; results begin as what no result is.  Test infrastructure only.
 // Usage: teacher_driver quantise MODE ROWS COLUMNS PAD
 //        teacher_driver product MODE ROWS WIDE OUTPUTS PAD TILE       (TILE: shim::force)
+//        teacher_driver scales MODE ROWS WIDE OUTPUTS PAD TILE        (scales next to their ends)
 //        teacher_driver top MODE ROWS COLUMNS K PAD KIND              (KIND 0 noise, 1 all equal, 2 masked but for few,
 //                                                                      10 ... all but the last K that many T below them,
 //                                                                      -10 ... one of these, the others 5 T further down)
@@ -134,10 +135,23 @@ void fill(const Room &q, const Room &s)
     }
 }
 
-void product(ccdc_block_t *b, int64_t rows, int64_t wide, int64_t outputs, int64_t pad)
+// Scales of a row next to one of ten places of their range, numbers of 8 bits of every size.
+void fill_ends(const Room &q, const Room &s, bool back)
+{
+    static constexpr int places[] = {0, 3, 8, 11, 60, 127, 200, 245, 248, 254};
+    for (int64_t i = 0; i < q.rows; i++) {
+        for (int64_t j = 0; j < q.columns; j++) q.as<unsigned char>(i, j) = (unsigned char)((int)(63 + 63 * uniform()) | (uniform() < 0 ? 128 : 0));
+        const int place = places[back ? 9 - i % 10 : i % 10];
+        for (int64_t k = 0; k < s.columns; k++)
+            s.as<unsigned char>(i, k) = k < q.columns / 128 ? (unsigned char)std::clamp<int>(place + (int)(i + 3 * k) % 5 - 2, 0, 254) : 255;
+    }
+}
+
+void product(ccdc_block_t *b, int64_t rows, int64_t wide, int64_t outputs, int64_t pad, bool ends)
 {
     Room x(rows, wide, 0, 1), xs(rows, kept(wide), 0, 1), w(outputs, wide, 0, 1), ws(outputs, kept(wide), 0, 1), y(rows, outputs, pad, elem(), 0xFF);
-    fill(x, xs), fill(w, ws);
+    if (ends) fill_ends(x, xs, false), fill_ends(w, ws, true);
+    else fill(x, xs), fill(w, ws);
     CHECK(ccdc_packed_product(b, rows, outputs, wide, x.p, xs.p, w.p, ws.p, y.p, y.ld, nullptr));
     for (int64_t i = 0; i < rows; i++)
         for (int64_t j = 0; j < outputs; j++) {
@@ -147,9 +161,13 @@ void product(ccdc_block_t *b, int64_t rows, int64_t wide, int64_t outputs, int64
                                  std::exp2(xs.as<unsigned char>(i, k / 128) + ws.as<unsigned char>(j, k / 128) - 254);
                 sum += t, size += std::fabs(t);
             }
+            // (what no number of the results' type holds, a part of the sum maybe, is not looked at)
+            if (ends && !(size < (mode == CCDC_F16_SUM_XOR ? 60000 : 0x1p127))) continue;
+            // (next to zero half of the least step: of fp32 in each addition, of the results' type in the rounding)
+            const double least = !ends ? 0.0 : (double)wide * 0x1p-150 + (mode == CCDC_F16_SUM_XOR ? 0x1p-25 : mode == CCDC_BF16_SUM_XOR ? 0x1p-134 : 0x1p-150);
             // binary16 has an infinity from 65520 on
             if (mode == CCDC_F16_SUM_XOR && std::fabs(sum) >= 65520) sum = std::copysign(INFINITY, sum);
-            near("y", i, j, get(y.at(i, j)), sum, (double)wide * 0x1p-24 * size + half_step() * std::fabs(sum) * 1.01);
+            near("y", i, j, get(y.at(i, j)), sum, (double)wide * 0x1p-24 * size + half_step() * std::fabs(sum) * 1.01 + least);
         }
 }
 
@@ -245,10 +263,11 @@ int main(int argc, char **argv)
     const std::string what = argv[1];
     const auto number = [&](int i) { return i < argc ? std::atoll(argv[i]) : 0ll; };
     mode = (int)number(2);
-    if (what == "product") shim::force = (int)number(7);
+    const bool ends = what == "scales";
+    if (what == "product" || ends) shim::force = (int)number(7);
     ccdc_block_t *b = make();
     if (what == "quantise") quantise(b, number(3), number(4), number(5));
-    else if (what == "product") product(b, number(3), number(4), number(5), number(6));
+    else if (what == "product" || ends) product(b, number(3), number(4), number(5), number(6), ends);
     else if (what == "top") top(b, number(3), number(4), (int)number(5), number(6), (int)number(7));
     else distill(b, number(3), number(4), (int)number(5), number(6), number(7) != 0);
     ccdc_block_destroy(b);
