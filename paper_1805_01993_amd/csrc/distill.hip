@@ -267,8 +267,9 @@ int by_columns(int64_t columns, int64_t rows, F launch)
     if constexpr (T::planes == 1) {
         if (packs <= 8192) return launch(sixteen, four, four, std::false_type());
         if (packs <= kMostHeld) return launch(sixteen, four, std::integral_constant<int, 3>(), std::true_type());
+    } else {
+        if (packs <= 8192) return go(sixteen, eight);
     }
-    if (packs <= 8192) return go(sixteen, eight);
     return launch(sixteen, std::integral_constant<int, 0>(), std::integral_constant<int, 0>(), std::true_type());
 }
 

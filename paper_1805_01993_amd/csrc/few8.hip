@@ -206,7 +206,8 @@ int run_few8(const Product8Args &a, hipStream_t st)
     const bool wide = a.rows_n >= 8192;               // with two groups a workgroup there still are enough workgroups
     if (a.rows_m <= 4 && a.rows_n < 2048) return go(four, one, four, one, two);
     if (a.rows_m <= 8) return wide ? go(two, one, eight, two, two) : go(two, one, eight, one, two);
-    if (wide && a.rows_m <= 32) return a.rows_m <= 16 ? go(one, one, four, four, two) : go(one, two, eight, two, two);
+    if constexpr (T::planes == 3)                     // (16-bit results go by tiles there)
+        if (wide) return a.rows_m <= 16 ? go(one, one, four, four, two) : go(one, two, eight, two, two);
     // the fewest rows, of both sides, that a CU has to read (what it takes from L2 or memory is some 45 GB/s)
     const auto read = [&](uint32_t n, uint32_t m) { return cdiv((uint64_t)cdiv(a.rows_n, n) * cdiv(a.rows_m, m), 256) * (n + m); };
     const auto small = read(8, 8), square = read(16, 16), tall = read(16, 32), large = read(32, 32), least = std::min(std::min(small, square), std::min(tall, large));
