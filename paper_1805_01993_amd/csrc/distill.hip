@@ -85,14 +85,19 @@ __global__ __launch_bounds__(64 * WAVES, LDS > 0 ? 8 : 0) void k_distill(const D
 #pragma unroll
         for (int h = 0; h < 2; h++)
             if (column[h] >= 0) {
-                t[h] = a.value[row * a.k + lane + 64 * h] * a.per_T;
+                t[h] = a.value[row * a.k + lane + 64 * h];
                 logit[h] = T::widen(((const E *)a.z)[row * a.ldz + column[h]]);
                 count += 1.0f;
                 most = fmaxf(most, logit[h]);
             }
-        // the teacher's p over the list and the rest
-        const float rest = a.rest ? a.rest[row] : -INFINITY;
-        const float top = fmaxf(fmaxf(wave_most(fmaxf(t[0], t[1])), rest), kLowest);
+        // the teacher's p over the list and the rest, all as distances from its largest value there: these by 1 / T round to what counts, where
+        // values far from zero would first (10000 / 0.7: p off by 5e-4), or pass fp32's range
+        const float value = wave_most(fmaxf(t[0], t[1])), largest = fmaxf(value, kLowest);
+#pragma unroll
+        for (int h = 0; h < 2; h++) t[h] = (t[h] - largest) * a.per_T;
+        float rest = a.rest ? a.rest[row] : -INFINITY;
+        if (fabsf(rest) < INFINITY) rest = fminf(fmaf(-largest, a.per_T, rest), -kLowest);
+        const float top = fmaxf(fmaxf(value > -INFINITY ? 0.0f : -INFINITY, rest), kLowest);
         float sum = 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; h++) sum += exponential(t[h] - top);
