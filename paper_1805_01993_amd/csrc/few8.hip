@@ -10,8 +10,9 @@
 // groups where that leaves enough workgroups; and scales are read a word of four at a time, or they are a third of the loads.  One row, 4096 x
 // 11264 (46 MB): one group, a scale at a time 14.8 us, two groups 11.1, and words 10.7 (4.3 TB/s; a kernel that does nothing takes 2).
 // From 9 rows on LDS's copies are worth their way where the weights have many rows (16 rows of 4096 x 11264: 15.3 us here, 14.6 by
-// tiles of 64 x 64; of 1600 x 32768 15.3, 12.4; of 11264 x 4096 13.7, 32), with fp32 results not (15.4, 21.9).  Loads of a next
-// step begun before this one's products lost more by those past the rows' ends than they gave (14.8 us).
+// tiles of 64 x 64; of 1600 x 32768 15.3, 12.4; of 11264 x 4096 13.7, 32).  With fp32 results rows go by here up to 32 and,
+// of few outputs, 64 (4096 x 11264, 16 rows 13.9 us, tiles 21.9; 32 rows 21.1, 22.1; 64 of 11264 x 4096 23.0, 55; but 24 of 1600 x 32768 21.0, 13.5).
+// Loads of a next step begun before this one's products lost more by those past the rows' ends than they gave (14.8 us).
 // Of few outputs there are fewer workgroups than CUs, and more than 16 rows are divided among workgroups too: a group of 8 or 16 outputs
 // for 8, 16 or 32 rows, whichever leaves a CU the least to read.  64 rows of 11264 x 1024 12.2 us by 16 x 16 (16 x 32 18.2, 8 x 8 22.4, tiles of
 // 64 x 64 31.5), x 2048 19.3 by 16 x 32 (32.0 by tiles), x 4096 25.0 by 32 x 32 (34.0), x 6000 34.6 by tiles (45.4); 16 rows of 11264 x

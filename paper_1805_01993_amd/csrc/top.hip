@@ -5,8 +5,8 @@
 // twenty bits of it.  What reaches it is put into a list in LDS, whatever the order, and ranked there: as keys of 64 bits, value then
 // column, no two are equal, so the order is one.  Where the list is long for its k (short rows of which much is wanted) the k-th
 // largest in it is found first, by ballots, bit by bit.  Where there is no room for all that reaches the bound (many equal values, those
-// of a mask by the lowest number among them) the row is counted again by digits of eight bits of those keys, values first and then
-// columns, until what is left has room.
+// of a mask by the lowest number among them; rows of 513 to 1024 columns with k above the 64 threads that they have, which give no
+// bound then) the row is counted again by digits of eight bits of those keys, values first and then columns, until what is left has room.
 #include "vocabulary.hpp"
 
 namespace {
@@ -286,8 +286,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_top(const TopArgs a)
 // rounds over LDS to share (us, bf16, k = 32; 16384 x 1000 by 1 wavefront of 2 packs 20.8, by 2 of 1 33.8; x 2000 by 1 of 4 32.2, by 4 of 2
 // 58.7; 15625 x 16000 by 4 of 8 132, by 8 of 4 144; 4997 x 50021 by 8 of 16 180, by 16 of 8 275, read again and again 237), a few rows by as
 // many as shorten their way (128 x 2000 7.9, 5.8; x 16000 9.5, 8.2; x 64000 15.3, 14.0).  Of one wavefront's 64 largest values, or two's 128, a
-// bound for many is too low (8192 x 2000, k = 64: 37 by one, 29 by four; x 4000, k = 128: 85 by two, 54 by four).  fp32 rows of more than
-// 65536 columns are not held (1923 x 130000 335, held 551).
+// bound for many is too low (8192 x 2000, k = 64: 37 by one, 29 by four; x 4000, k = 128: 85 by two, 54 by four).  Of rows of up
+// to 1024 columns that is not measured (8192 x 1000 by one wavefront: k = 64 28, 65 34, 128 42).  fp32 rows of more than 65536 columns are not held (1923 x 130000 335, held 551).
 template <class T, class F>
 int by_columns(int64_t columns, int64_t rows, int k, F launch)
 {
