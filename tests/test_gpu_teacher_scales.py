@@ -23,7 +23,7 @@ def matrix(seed, rows, wide, centres):
 
 
 @pytest.mark.parametrize("mode", MODES)
-@pytest.mark.parametrize("rows,wide,outputs", [(1, 128, 10), (2, 128, 11), (9, 640, 23), (1, 1152, 20), (4, 1152, 31), (8, 1024, 40), (13, 1152, 24), (24, 1152, 70), (60, 1152, 33),
+@pytest.mark.parametrize("rows,wide,outputs", [(1, 128, 10), (2, 128, 11), (9, 640, 23), (1, 1152, 20), (4, 1152, 31), (8, 1024, 40), (13, 1152, 24), (24, 1152, 70), (60, 1152, 33), (3, 1152, 8195), (12, 1152, 8197), (20, 1152, 8195),
                                                (70, 128, 30), (80, 640, 70), (300, 384, 140)])
 def test_product_with_scales_next_to_their_ends(blocks, mode, rows, wide, outputs):  # noqa: F811
     """Every pair of ends; compared are those whose products a number of the results' type can hold."""
